@@ -105,6 +105,7 @@ extern "C" {
 #define DFLOW_STATUS_BAD_TOKEN 1
 #define DFLOW_STATUS_CAPACITY 2
 #define DFLOW_STATUS_BAD_PAGE 4
+#define DFLOW_STATUS_BAD_SLOT 8
 
 typedef struct dflow_dims {
   int dtype;              /* DFLOW_F32 or DFLOW_BF16 */
@@ -405,6 +406,99 @@ int dflow_move_slot(dflow_ctx* ctx, hipStream_t stream, int from, int to);
 int dflow_bench_force_drafts(dflow_ctx* ctx, hipStream_t stream, int nseq, const int32_t* traj, int traj_stride,
                              int traj_len, const int8_t* mode, const int32_t* tok, const int32_t* anchor,
                              const int32_t* start_pos, int32_t* block_tok);
+
+/* ---- Paged KV cache in 8 bits: page tables sized to the requests, the append
+ * and the attention that reads it.  These calls need no context; each takes its
+ * buffers, and the device status word, from the caller.
+ *
+ * A layer's cache holds e4m3 codes with one fp32 scale per group of 16 tokens,
+ * kv head, and keys or values; a value is code * scale.  Position p of a
+ * sequence lies in page page_table[p/64], token p%64, group p%64/16.  Half the
+ * bytes of the bf16 cache. */
+typedef struct dflow_kv8 {
+  void* k;                /* e4m3 [num_pages][n_kv_heads][64][head_dim], 16-byte aligned */
+  void* v;                /* e4m3 [num_pages][n_kv_heads][head_dim][64] (channel by channel), 16-byte aligned */
+  float* k_scale;         /* [num_pages][n_kv_heads][4], positive where the group holds tokens */
+  float* v_scale;
+  int num_pages;          /* at most 2^31 / 64 - 1 */
+  int n_kv_heads;
+  int head_dim;           /* 64 or 128 */
+} dflow_kv8;
+
+/* Pages of a batch and the pool they come from.  Row s of page_table holds the
+ * pages of sequence s in order, n_held[s] of them; free_pages is a stack of
+ * the n_free[0] unused page ids, its top at n_free[0] - 1. */
+typedef struct dflow_page_pool {
+  int32_t* page_table;    /* [nseq][max_pages] */
+  int max_pages;
+  int32_t* n_held;        /* [nseq] */
+  int32_t* free_pages;    /* [num_pages] */
+  int num_pages;
+  int32_t* n_free;        /* [1] */
+} dflow_page_pool;
+
+/* Sizes every row of the page table to its request and maps the new tokens to
+ * cache slots, on the device.  Sequence s (of at most 1024) holds seq_len[s]
+ * tokens and is about to take new_len[s] more (new_len NULL: none); afterwards
+ * its row has ceil((seq_len + new_len) / 64) pages.  First every row that has more
+ * gives the pages above back (its entries become -1), then rows that need pages take
+ * them from the top of the stack in sequence order.  Growing and shrinking back
+ * restores the stack.  A sequence that does not fit -- the pool cannot serve
+ * it and all before it, the row is too short, a negative length -- keeps its
+ * row, gets no slots (-1) and sets DFLOW_STATUS_CAPACITY; no later sequence
+ * takes pages past it.
+ * slot (nullable): the new tokens' slots, sequence after sequence:
+ * slot[row_start[s] + j] = 64 * page + token of position seq_len[s] + j, with
+ * row_start [nseq + 1] (written; required with slot) the running sum of
+ * new_len.  At most slot_cap slots are written; more new tokens than that
+ * cut row_start at slot_cap and set DFLOW_STATUS_CAPACITY.  Slots behind the
+ * last sequence's are left as they were.  A page id outside the pool gives -1. */
+int dflow_page_resize(hipStream_t stream, const dflow_page_pool* pool, int nseq, const int32_t* seq_len,
+                      const int32_t* new_len, int32_t* slot, int slot_cap, int32_t* row_start, int32_t* status);
+
+/* Writes rows of keys and values to their slots.  k, v: [rows][n_kv_heads]
+ * [head_dim] in the storage type, rows ld_k / ld_v elements apart (16-byte
+ * aligned, a multiple of 16 bytes).  slot [rows]: 64 * page + token, or -1 for a
+ * row that is not written.
+ * The rows of a group of 16 tokens are consecutive (no row without a slot
+ * between them) and ascending, as dflow_page_resize maps them: a group that a
+ * call comes back to ends with unspecified values.  Tokens of the
+ * group below its first appended one belong to the sequence and keep their
+ * values; tokens behind are left as they were, no part of the sequence.  The
+ * group's scale becomes the smallest power of two, 2^-100 to 2^120, that brings
+ * the largest finite magnitude of kept and appended values to 448 or less (1 if all
+ * are zero); codes are rounded to nearest even, infinities saturate, NaN stays
+ * NaN.  A slot outside the cache, or one that does not ascend from the row
+ * before it in the same group, is skipped and sets DFLOW_STATUS_BAD_SLOT. */
+int dflow_kv8_append(hipStream_t stream, int dtype, const dflow_kv8* cache, int rows, const void* k, size_t ld_k,
+                     const void* v, size_t ld_v, const int32_t* slot, int32_t* status);
+
+/* Bytes of workspace a dflow_kv8_attention call of these sizes needs on the
+ * current device (0: none); (size_t)-1 if an argument is invalid. */
+size_t dflow_kv8_attention_workspace(int dtype, int nseq, int max_rows, int max_len, int n_heads, int n_kv_heads,
+                                     int head_dim);
+
+/* Attention of a ragged batch over the 8-bit cache.  Sequence s has rows
+ * row_start[s] .. row_start[s + 1] - 1 of q and out ([rows][n_heads][head_dim] in the
+ * storage type, ld_q / ld_out elements apart, 16-byte aligned, a multiple of 16
+ * bytes) and kv_len[s] cached tokens, the rows' own among them: row j of n is
+ * at position kv_len[s] - n + j.  causal != 0: a row sees the keys up to its
+ * position; 0: all kv_len[s].  out = softmax(scale q.k) v over the keys it sees, 0 for
+ * a row that sees none; other rows of out are left as they were.
+ * max_rows bounds the rows of a sequence and max_len the cached tokens (host
+ * values, which size the launch; with the batch size they fix how a sequence is
+ * split, so a row's result does not depend on the other sequences).  Rows past
+ * max_rows are not computed and keys past max_len or the page table not read,
+ * a row_start outside 0..rows skips the sequence; each sets
+ * DFLOW_STATUS_CAPACITY.  Keys of a page whose id is outside the pool are not
+ * seen (DFLOW_STATUS_BAD_PAGE).  Bytes behind a sequence's end may be anything.
+ * Scores, sums and outputs are held in fp32; bf16 rows round probabilities to 11
+ * bits, fp32 rows to 22.  workspace: device, 16-byte aligned, used by one call
+ * at a time (calls and graphs that share it must not overlap). */
+int dflow_kv8_attention(hipStream_t stream, int dtype, const dflow_kv8* cache, int nseq, const int32_t* page_table,
+                        int max_pages, const int32_t* kv_len, const int32_t* row_start, int rows, int max_rows,
+                        int max_len, int n_heads, const void* q, size_t ld_q, float scale, int causal, void* out,
+                        size_t ld_out, void* workspace, size_t workspace_bytes, int32_t* status);
 
 /* Kernel timing (tracing aid, not part of the method).  While enabled, every
  * weight-streaming GEMM launch and every attention launch is bracketed by HIP

@@ -6,3 +6,4 @@ marshals arguments, allocates device memory through PyTorch and sequences
 the four round calls.
 """
 from .runtime import DFlowError, Runtime, library_path, load_library  # noqa: F401
+from .kv8 import KV8Cache, PagePool  # noqa: F401

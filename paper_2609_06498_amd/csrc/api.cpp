@@ -3,6 +3,8 @@
 // Every computation is a HIP kernel launch on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -13,6 +15,7 @@
 #include "../../include/dflow.h"
 #include "common.h"
 #include "kernels.h"
+#include "kv8.h"
 #include "round_state.h"
 
 using namespace dflow;
@@ -1017,6 +1020,171 @@ extern "C" int kv_commit(dflow_ctx* c, hipStream_t st, int nseq, const int32_t* 
   c->phase = DFLOW_PHASE_COMMIT;
   HIPCHK(ctx_append(c, st, nseq, c->dm.block, seq_len, accept_len, c->c.page_table));
   HIPCHK(launch_commit(accept_len, nseq, seq_len, st));
+  return DFLOW_OK;
+}
+
+// ------------------------------------------------------------------ paged 8-bit cache
+namespace {
+
+// compute units of the current device (asked for once per device)
+int device_cus(int* cus) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  HIPCHK(hipGetDevice(&dev));
+  int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (n < 1) {
+    HIPCHK(hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev));
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+  }
+  *cus = n;
+  return DFLOW_OK;
+}
+
+int kv8_cache(const char* who, const dflow_kv8* k, Kv8Cache* c) {
+  if (!k || !k->k || !k->v || !k->k_scale || !k->v_scale) return fail(DFLOW_EINVAL, "%s: null cache pointer", who);
+  if (k->head_dim != 64 && k->head_dim != 128) return fail(DFLOW_ESHAPE, "%s: head_dim %d (64 or 128)", who, k->head_dim);
+  if (k->n_kv_heads < 1 || k->n_kv_heads > 1024) return fail(DFLOW_ESHAPE, "%s: %d kv heads", who, k->n_kv_heads);
+  if (k->num_pages < 1 || k->num_pages > INT_MAX / PAGE)
+    return fail(DFLOW_ECAPACITY, "%s: %d pages (1..%d)", who, k->num_pages, INT_MAX / PAGE);
+  if (((uintptr_t)k->k | (uintptr_t)k->v) & 15 || ((uintptr_t)k->k_scale | (uintptr_t)k->v_scale) & 3)
+    return fail(DFLOW_EINVAL, "%s: keys and values must be 16-byte and scales 4-byte aligned", who);
+  *c = Kv8Cache{(uint8_t*)k->k, (uint8_t*)k->v, k->k_scale, k->v_scale, k->num_pages, k->n_kv_heads, k->head_dim};
+  return DFLOW_OK;
+}
+
+// a matrix of rows: 16-byte aligned, rows at least `width` elements and a multiple of 16 bytes apart
+int kv8_rows_arg(const char* who, const char* what, int dtype, const void* p, size_t ld, size_t width) {
+  const size_t elt = dtype == DFLOW_BF16 ? 2 : 4;
+  if (!p) return fail(DFLOW_EINVAL, "%s: %s is null", who, what);
+  if (((uintptr_t)p & 15) || ld < width || ld * elt % 16)
+    return fail(DFLOW_ESHAPE, "%s: %s must be 16-byte aligned with rows a multiple of 16 bytes and at least %zu elements "
+                              "apart (row stride %zu)", who, what, width, ld);
+  return DFLOW_OK;
+}
+
+}  // namespace
+
+extern "C" int dflow_page_resize(hipStream_t st, const dflow_page_pool* pool, int nseq, const int32_t* seq_len,
+                                 const int32_t* new_len, int32_t* slot, int slot_cap, int32_t* row_start,
+                                 int32_t* status) {
+  if (!pool || !pool->page_table || !pool->n_held || !pool->free_pages || !pool->n_free)
+    return fail(DFLOW_EINVAL, "page_resize: null pool pointer");
+  if (!seq_len || !status) return fail(DFLOW_EINVAL, "page_resize: null argument");
+  if (nseq < 1 || nseq > PAGES_MAX_SEQ)
+    return fail(DFLOW_ECAPACITY, "page_resize: nseq %d outside 1..%d", nseq, PAGES_MAX_SEQ);
+  if (pool->max_pages < 1 || pool->max_pages > INT_MAX / PAGE || pool->num_pages < 1 ||
+      pool->num_pages > INT_MAX / PAGE)
+    return fail(DFLOW_ECAPACITY, "page_resize: max_pages %d, num_pages %d (1..%d)", pool->max_pages, pool->num_pages,
+                INT_MAX / PAGE);
+  if (slot && (!new_len || !row_start)) return fail(DFLOW_EINVAL, "page_resize: a slot map needs new_len and row_start");
+  if (slot_cap < 0) return fail(DFLOW_ESHAPE, "page_resize: slot_cap %d", slot_cap);
+  PageResizeParams p{};
+  p.nseq = nseq;
+  p.seq_len = seq_len;
+  p.new_len = new_len;
+  p.page_table = pool->page_table;
+  p.max_pages = pool->max_pages;
+  p.num_pages = pool->num_pages;
+  p.n_held = pool->n_held;
+  p.free_pages = pool->free_pages;
+  p.n_free = pool->n_free;
+  p.slot = slot;
+  p.slot_cap = slot_cap;
+  p.row_start = row_start;
+  p.status = status;
+  HIPCHK(launch_page_resize(p, st));
+  return DFLOW_OK;
+}
+
+extern "C" int dflow_kv8_append(hipStream_t st, int dtype, const dflow_kv8* cache, int rows, const void* k, size_t ld_k,
+                                const void* v, size_t ld_v, const int32_t* slot, int32_t* status) {
+  Kv8AppendParams p{};
+  int rc = kv8_cache("kv8_append", cache, &p.c);
+  if (rc) return rc;
+  if (dtype != DFLOW_F32 && dtype != DFLOW_BF16) return fail(DFLOW_EDTYPE, "kv8_append: dtype %d", dtype);
+  if (rows < 0) return fail(DFLOW_ESHAPE, "kv8_append: %d rows", rows);
+  if (!status || (rows > 0 && !slot)) return fail(DFLOW_EINVAL, "kv8_append: null argument");
+  if (rows == 0) return DFLOW_OK;
+  const size_t width = (size_t)p.c.Hkv * p.c.Dh;
+  if ((rc = kv8_rows_arg("kv8_append", "k", dtype, k, ld_k, width))) return rc;
+  if ((rc = kv8_rows_arg("kv8_append", "v", dtype, v, ld_v, width))) return rc;
+  p.k = k;
+  p.v = v;
+  p.ld_k = ld_k;
+  p.ld_v = ld_v;
+  p.slot = slot;
+  p.rows = rows;
+  p.status = status;
+  HIPCHK(launch_kv8_append(dtype == DFLOW_BF16, p, st));
+  return DFLOW_OK;
+}
+
+namespace {
+int kv8_geometry(const char* who, int dtype, int nseq, int max_rows, int max_len, int n_heads, int n_kv_heads) {
+  if (dtype != DFLOW_F32 && dtype != DFLOW_BF16) return fail(DFLOW_EDTYPE, "%s: dtype %d", who, dtype);
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || n_heads > 16384)
+    return fail(DFLOW_ESHAPE, "%s: heads %d / kv heads %d", who, n_heads, n_kv_heads);
+  if (nseq < 1 || nseq > 65535) return fail(DFLOW_ECAPACITY, "%s: nseq %d outside 1..65535", who, nseq);
+  if (max_rows < 0 || max_rows > (1 << 20) || max_len < 0)
+    return fail(DFLOW_ESHAPE, "%s: max_rows %d (0..2^20), max_len %d", who, max_rows, max_len);
+  return DFLOW_OK;
+}
+}  // namespace
+
+extern "C" size_t dflow_kv8_attention_workspace(int dtype, int nseq, int max_rows, int max_len, int n_heads,
+                                                int n_kv_heads, int head_dim) {
+  int cus = 0;
+  if (kv8_geometry("kv8_attention_workspace", dtype, nseq, max_rows, max_len, n_heads, n_kv_heads)) return (size_t)-1;
+  if (head_dim != 64 && head_dim != 128) {
+    fail(DFLOW_ESHAPE, "kv8_attention_workspace: head_dim %d (64 or 128)", head_dim);
+    return (size_t)-1;
+  }
+  if (device_cus(&cus)) return (size_t)-1;
+  return max_rows < 1 ? 0 : kv8_attn_workspace(dtype == DFLOW_BF16, nseq, max_rows, max_len, n_heads, n_kv_heads,
+                                               head_dim, cus);
+}
+
+extern "C" int dflow_kv8_attention(hipStream_t st, int dtype, const dflow_kv8* cache, int nseq, const int32_t* page_table,
+                                   int max_pages, const int32_t* kv_len, const int32_t* row_start, int rows,
+                                   int max_rows, int max_len, int n_heads, const void* q, size_t ld_q, float scale,
+                                   int causal, void* out, size_t ld_out, void* workspace, size_t workspace_bytes,
+                                   int32_t* status) {
+  Kv8AttnParams p{};
+  int rc = kv8_cache("kv8_attention", cache, &p.c);
+  if (rc) return rc;
+  if ((rc = kv8_geometry("kv8_attention", dtype, nseq, max_rows, max_len, n_heads, p.c.Hkv))) return rc;
+  if (!page_table || !kv_len || !row_start || !status) return fail(DFLOW_EINVAL, "kv8_attention: null argument");
+  if (max_pages < 1 || max_pages > INT_MAX / PAGE) return fail(DFLOW_ECAPACITY, "kv8_attention: max_pages %d", max_pages);
+  if (rows < 0) return fail(DFLOW_ESHAPE, "kv8_attention: %d rows", rows);
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(DFLOW_EINVAL, "kv8_attention: scale %g (must be positive)", scale);
+  if (rows == 0 || max_rows == 0) return DFLOW_OK;
+  const size_t width = (size_t)n_heads * p.c.Dh;
+  if ((rc = kv8_rows_arg("kv8_attention", "q", dtype, q, ld_q, width))) return rc;
+  if ((rc = kv8_rows_arg("kv8_attention", "out", dtype, out, ld_out, width))) return rc;
+  if ((rc = device_cus(&p.cus))) return rc;
+  p.key_cap = (long long)max_len < (long long)max_pages * PAGE ? max_len : max_pages * PAGE;
+  const size_t need = kv8_attn_workspace(dtype == DFLOW_BF16, nseq, max_rows, p.key_cap, n_heads, p.c.Hkv, p.c.Dh, p.cus);
+  if (need > 0 && (!workspace || ((uintptr_t)workspace & 15)))
+    return fail(DFLOW_EINVAL, "kv8_attention: workspace must be given and 16-byte aligned");
+  if (workspace_bytes < need)
+    return fail(DFLOW_ECAPACITY, "kv8_attention: workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  p.page_table = page_table;
+  p.kv_len = kv_len;
+  p.row_start = row_start;
+  p.q = q;
+  p.out = out;
+  p.ld_q = ld_q;
+  p.ld_out = ld_out;
+  p.scale = scale;
+  p.nseq = nseq;
+  p.rows = rows;
+  p.max_rows = max_rows;
+  p.Hq = n_heads;
+  p.max_pages = max_pages;
+  p.causal = causal != 0;
+  p.part = (float*)workspace;
+  p.status = status;
+  HIPCHK(launch_kv8_attention(dtype == DFLOW_BF16, p, st));
   return DFLOW_OK;
 }
 

@@ -68,6 +68,7 @@ template <> struct Chunk<float> {
 }  // namespace dflow
 
 #include "attn_prefill.h"
+#include "kv8_attention.h"
 
 namespace dflow {
 

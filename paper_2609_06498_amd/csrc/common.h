@@ -298,6 +298,7 @@ enum : int {
   ST_BAD_TOKEN = 1,        // token id outside [0, V)
   ST_CAPACITY = 2,         // a position beyond the sequence's page table
   ST_BAD_PAGE = 4,         // page id outside the pool
+  ST_BAD_SLOT = 8,         // cache slot outside the pool, or not ascending within its group
 };
 __device__ inline void set_status(int* status, int bit) { atomicOr(status, bit); }
 

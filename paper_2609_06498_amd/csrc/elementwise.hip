@@ -591,3 +591,5 @@ hipError_t launch_fill_u32(uint32_t* dst, uint32_t value, size_t n, hipStream_t 
 }
 
 }  // namespace dflow
+
+#include "kv8_cache.h"

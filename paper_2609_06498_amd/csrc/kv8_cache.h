@@ -1,0 +1,343 @@
+// Writes of the paged 8-bit cache and its page table (included by elementwise.hip).
+#pragma once
+#include "common.h"
+#include "kernels.h"
+#include "kv8.h"
+
+namespace dflow {
+
+// ---------------------------------------------------------------- append
+// Key and value rows go to their slots in e4m3 with one power-of-two scale per
+// 16 tokens and head: s = the smallest power of two with max|x| / s <= 448 over
+// the group's kept tokens (those below the first appended one: they belong to the
+// sequence already) and the appended ones.  Dividing by a power of two is exact,
+// so kept codes move to a new scale exactly (apart from values that become
+// subnormal), and a group filled token by token ends as one filled at once.
+// Tokens behind the appended ones are left as they were.
+//
+// The rows of a run (consecutive rows of one group, ascending) are one wave's
+// work, keys and values apart, a kv head each.  A key wave holds a quarter of a
+// token's channels per lane; a value wave DH / 64 channels of all 16 tokens, whose
+// codes are one 16-byte store per channel (values lie channel by channel).  Bound
+// by memory: rows read once, codes written once; for many rows a workgroup takes
+// 4 RC consecutive rows of one head, so that the value stores of a page's four
+// groups meet in one cache.
+
+// 2^e of the scale rule for a maximum of finite magnitudes (0: scale 1)
+__device__ inline int kv8_exponent(float amax) {
+  if (!(amax > 0.f)) return 0;
+  int e;
+  const float m = frexpf(amax, &e);            // amax = m 2^e, m in [1/2, 1); 448 = 7/8 2^9
+  e = e - 9 + (m > 0.875f ? 1 : 0);
+  return min(max(e, KV8_MIN_EXP), KV8_MAX_EXP);
+}
+__device__ inline float kv8_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+__device__ inline float kv8_finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.f;               // infinities and NaN do not set a scale
+}
+// four values / 2^e as e4m3 codes: nearest even, at most 448 in magnitude, NaN stays NaN
+__device__ inline uint32_t kv8_pack4(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float v = x[i] * inv;
+    y[i] = v == v ? fminf(fmaxf(v, -448.f), 448.f) : v;
+  }
+  int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+}
+__device__ inline void kv8_unpack4(uint32_t u, float scale, float* x) {
+  x[0] = __builtin_amdgcn_cvt_f32_fp8(u, 0) * scale;
+  x[1] = __builtin_amdgcn_cvt_f32_fp8(u, 1) * scale;
+  x[2] = __builtin_amdgcn_cvt_f32_fp8(u, 2) * scale;
+  x[3] = __builtin_amdgcn_cvt_f32_fp8(u, 3) * scale;
+}
+
+template <typename T, int DH, int RC>
+__global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
+  static_assert(RC + 17 <= 64, "a lane per row of the window");
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool is_v = blockIdx.y & 1;
+  const int h = blockIdx.y >> 1;
+  const int r0 = (blockIdx.x * 4 + w) * RC;
+  if (r0 >= p.rows) return;                    // uniform per wave
+  // slots of rows r0 - 1 (lane 0) .. r0 + RC + 15
+  const int row = r0 - 1 + lane;
+  const int cap = p.c.num_pages * PAGE;
+  int slot = row >= 0 && row < p.rows && lane < RC + 17 ? p.slot[row] : -1;
+  bool fault = slot < -1 || slot >= cap;
+  if (fault) slot = -1;
+  const int group = slot < 0 ? -1 - lane : slot / KV8_GROUP;     // (no two invalid rows share a group)
+  const int before = __shfl_up(group, 1, 64), sbefore = __shfl_up(slot, 1, 64);
+  const bool mine = lane >= 1 && lane <= RC;
+  const bool follows = lane >= 1 && slot >= 0 && group == before;
+  fault |= follows && slot <= sbefore;
+  if (blockIdx.y == 0 && __builtin_amdgcn_ballot_w64(mine && fault) != 0 && lane == 0) set_status(p.status, ST_BAD_SLOT);
+  uint64_t leads = __builtin_amdgcn_ballot_w64(mine && slot >= 0 && !follows);
+  while (leads) {                              // uniform
+    const int ld = __builtin_ctzll(leads);
+    leads &= leads - 1;
+    const int s0 = __builtin_amdgcn_readlane(slot, ld), gr = s0 / KV8_GROUP, t0 = s0 % KV8_GROUP;
+    // source row of each token of the group: lane t of src, -1: not appended
+    int src = -1, top = -1;
+#pragma unroll
+    for (int i = 0; i < KV8_GROUP; ++i) {
+      const int sl = ld + i < 64 ? __builtin_amdgcn_readlane(slot, (ld + i) & 63) : -1;
+      const int gi = ld + i < 64 ? __builtin_amdgcn_readlane(group, (ld + i) & 63) : -1;
+      if (gi != gr) break;
+      const int t = sl % KV8_GROUP;
+      if (t <= top) continue;                  // not ascending: skipped (status set above)
+      top = t;
+      if ((lane & 15) == t) src = r0 - 1 + ld + i;
+    }
+    const uint32_t fresh = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 16 && src >= 0);
+    const int page = gr / 4, part = gr % 4;
+    const size_t ph = (size_t)page * p.c.Hkv + h;
+    float* scale = (is_v ? p.c.vs : p.c.ks) + ph * 4 + part;
+    const float old = t0 > 0 ? *scale : 1.f;
+    if (!is_v) {
+      constexpr int CL = DH / 4;               // channels of a lane
+      const int t = lane >> 2, c0 = (lane & 3) * CL;
+      const int sr = __shfl(src, t, 64);
+      uint32_t* dst = reinterpret_cast<uint32_t*>(p.c.k + (ph * PAGE + part * KV8_GROUP + t) * DH + c0);
+      float x[CL];
+#pragma unroll
+      for (int i = 0; i < CL; ++i) x[i] = 0.f;
+      if (sr >= 0) {
+        const T* k = reinterpret_cast<const T*>(p.k) + (size_t)sr * p.ld_k + (size_t)h * DH + c0;
+#pragma unroll
+        for (int i = 0; i < CL; i += 16) Row16<T>::load(k + i, x + i);
+      } else if (t < t0) {
+#pragma unroll
+        for (int i = 0; i < CL; i += 16) {
+          const uint4 u = *reinterpret_cast<const uint4*>(dst + i / 4);
+          kv8_unpack4(u.x, old, x + i);
+          kv8_unpack4(u.y, old, x + i + 4);
+          kv8_unpack4(u.z, old, x + i + 8);
+          kv8_unpack4(u.w, old, x + i + 12);
+        }
+      }
+      float amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < CL; ++i) amax = fmaxf(amax, kv8_finite_abs(x[i]));
+      const int e = kv8_exponent(wave_max(amax));
+      const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
+      if (sr >= 0 || (t < t0 && sc != old)) {
+#pragma unroll
+        for (int i = 0; i < CL; i += 16)
+          *reinterpret_cast<uint4*>(dst + i / 4) =
+              make_uint4(kv8_pack4(x + i, inv), kv8_pack4(x + i + 4, inv), kv8_pack4(x + i + 8, inv),
+                         kv8_pack4(x + i + 12, inv));
+      }
+      if (lane == 0) *scale = sc;
+    } else {
+      constexpr int CL = DH / 64;
+      const int c0 = lane * CL;
+      uint8_t* dst = p.c.v + (ph * DH + c0) * PAGE + part * KV8_GROUP;
+      float x[CL][KV8_GROUP];
+      uint4 was[CL];
+#pragma unroll
+      for (int c = 0; c < CL; ++c) {
+        was[c] = make_uint4(0, 0, 0, 0);
+        if (fresh != 0xFFFFu) was[c] = *reinterpret_cast<const uint4*>(dst + c * PAGE);   // uniform
+      }
+#pragma unroll
+      for (int t = 0; t < KV8_GROUP; ++t) {
+        const int sr = __builtin_amdgcn_readlane(src, t);
+        if (sr >= 0) {
+          const T* v = reinterpret_cast<const T*>(p.v) + (size_t)sr * p.ld_v + (size_t)h * DH + c0;
+#pragma unroll
+          for (int c = 0; c < CL; ++c) x[c][t] = TT<T>::ld(v, c);
+        } else {
+          const uint32_t sel = t / 4;
+#pragma unroll
+          for (int c = 0; c < CL; ++c) {
+            const uint32_t u = sel == 0 ? was[c].x : sel == 1 ? was[c].y : sel == 2 ? was[c].z : was[c].w;
+            float y[4];
+            kv8_unpack4(u, old, y);
+            x[c][t] = t < t0 ? y[t & 3] : 0.f;
+          }
+        }
+      }
+      float amax = 0.f;
+#pragma unroll
+      for (int c = 0; c < CL; ++c)
+#pragma unroll
+        for (int t = 0; t < KV8_GROUP; ++t) amax = fmaxf(amax, kv8_finite_abs(x[c][t]));
+      const int e = kv8_exponent(wave_max(amax));
+      const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
+      const uint32_t live = fresh | ((1u << t0) - 1u);
+#pragma unroll
+      for (int c = 0; c < CL; ++c) {
+        uint32_t u[4], o[4] = {was[c].x, was[c].y, was[c].z, was[c].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t keep = 0;                   // bytes of the tokens that stay as they were
+#pragma unroll
+          for (int b = 0; b < 4; ++b) keep |= (live >> (4 * q + b)) & 1u ? 0u : 0xFFu << (8 * b);
+          u[q] = (kv8_pack4(&x[c][4 * q], inv) & ~keep) | (o[q] & keep);
+        }
+        *reinterpret_cast<uint4*>(dst + c * PAGE) = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+      if (lane == 0) *scale = sc;
+    }
+  }
+}
+
+template <typename T, int DH>
+static hipError_t launch_append_dh(const Kv8AppendParams& p, hipStream_t st) {
+  // A round's rows spread over as many waves as there are rows; from a few
+  // thousand rows on they are prompts, whose runs are 16 rows.
+  if (p.rows <= 2048)
+    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 1>), dim3((p.rows + 3) / 4, 2 * p.c.Hkv), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 32>), dim3((p.rows + 127) / 128, 2 * p.c.Hkv), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_append(bool isbf, const Kv8AppendParams& p, hipStream_t st) {
+  if (p.rows < 1) return hipSuccess;
+  if (p.c.Dh == 128) return isbf ? launch_append_dh<bf16, 128>(p, st) : launch_append_dh<float, 128>(p, st);
+  if (p.c.Dh == 64) return isbf ? launch_append_dh<bf16, 64>(p, st) : launch_append_dh<float, 64>(p, st);
+  return hipErrorInvalidValue;
+}
+
+// ---------------------------------------------------------------- pages
+// Rows of a page table resized to request lengths.  One workgroup, a thread per
+// sequence: target = ceil((len + new) / 64) pages; the pages above it go back to
+// the free stack, then rows take pages from its top, both placed by exclusive
+// sums over the sequences.  A page's place depends on its rank (by sequence, then
+// page): the lowest rank of the released ones ends on top, the lowest of the taken
+// ones is popped first, so growing and shrinking again restores the stack.
+// Slots are mapped here when they are few, else by a launch of their own that
+// spreads them over the chip.  Bound by latency (a few dependent loads and two
+// scans), or by the slot stores.
+constexpr int PAGES_T = 1024;
+constexpr int PAGES_INLINE_ROWS = 4096;
+
+// exclusive sum over the workgroup's threads; *total: the sum
+__device__ inline long long block_scan(long long v, long long* sh /* [17] */, long long* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) sh[w] = x;
+  __syncthreads();
+  long long base = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < PAGES_T / 64; ++i) {
+    if (i < w) base += sh[i];
+    all += sh[i];
+  }
+  *total = all;
+  return base + x - v;
+}
+
+// slot of row r of the call: sequence by binary search over the row starts
+__device__ inline int map_slot(const PageResizeParams& p, const int* starts, int r) {
+  int lo = 0, hi = p.nseq;                     // starts[lo] <= r < starts[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (starts[mid] <= r) lo = mid;
+    else hi = mid;
+  }
+  const long long len = p.seq_len[lo], nw = p.new_len[lo];
+  if (len < 0 || (len + nw + PAGE - 1) / PAGE > p.n_held[lo]) return -1;   // refused
+  const int pos = (int)len + r - starts[lo];
+  const int page = p.page_table[(size_t)lo * p.max_pages + pos / PAGE];
+  return page < 0 || page >= p.num_pages ? -1 : page * PAGE + pos % PAGE;
+}
+
+__global__ void __launch_bounds__(PAGES_T) page_resize_kernel(PageResizeParams p, int inline_slots) {
+  __shared__ long long sh[17];
+  __shared__ int s_held[PAGES_MAX_SEQ], s_cnt[PAGES_MAX_SEQ], s_off[PAGES_MAX_SEQ], s_start[PAGES_MAX_SEQ + 1];
+  const int s = threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const bool have = s < p.nseq;
+  const long long len = have ? p.seq_len[s] : 0, nw = have && p.new_len ? p.new_len[s] : 0;
+  const int top0 = *p.n_free;
+  int bits = top0 < 0 || top0 > p.num_pages ? ST_CAPACITY : 0;
+  const int top = min(max(top0, 0), p.num_pages);
+  const int held0 = have ? p.n_held[s] : 0;
+  int held = min(max(held0, 0), p.max_pages);
+  const long long target = (len + nw + PAGE - 1) / PAGE;
+  const bool valid = have && len >= 0 && nw >= 0 && target <= p.max_pages;
+  if ((have && !valid) || held != held0) bits |= ST_CAPACITY;
+  // give back
+  const int drop = valid && held > target ? held - (int)target : 0;
+  long long dropped;
+  int off = (int)block_scan(drop, sh, &dropped);
+  if (have) { s_held[s] = held - drop; s_cnt[s] = drop; s_off[s] = off; }
+  __syncthreads();
+  if (dropped > 0) {                           // uniform
+    for (int q = w; q < p.nseq; q += PAGES_T / 64)
+      for (int i = lane; i < s_cnt[q]; i += 64) {
+        int* e = p.page_table + (size_t)q * p.max_pages + s_held[q] + i;
+        const long long at = top + dropped - 1 - (s_off[q] + i);
+        if (at < p.num_pages) p.free_pages[at] = *e;
+        else bits |= ST_CAPACITY;              // more pages than the pool has: the caller's state is wrong
+        *e = -1;
+      }
+    __threadfence_block();
+  }
+  held -= drop;
+  const long long avail = min((long long)top + dropped, (long long)p.num_pages);
+  // take
+  const int want = valid && target > held ? (int)target - held : 0;
+  long long wanted;
+  const long long at = block_scan(want, sh, &wanted);     // (barriers: the pushes above are done)
+  const int take = want > 0 && at + want <= avail ? want : 0;
+  if (want > take) bits |= ST_CAPACITY;
+  long long taken;
+  block_scan(take, sh, &taken);
+  if (have) { s_held[s] = held; s_cnt[s] = take; s_off[s] = (int)at; }
+  __syncthreads();
+  if (taken > 0) {
+    for (int q = w; q < p.nseq; q += PAGES_T / 64)
+      for (int i = lane; i < s_cnt[q]; i += 64)
+        p.page_table[(size_t)q * p.max_pages + s_held[q] + i] = p.free_pages[avail - 1 - (s_off[q] + i)];
+  }
+  held += take;
+  if (have && held != held0) p.n_held[s] = held;
+  if (threadIdx.x == 0) *p.n_free = (int)(avail - taken);
+  if (p.slot) {
+    long long rows;
+    const long long r = block_scan(nw > 0 ? nw : 0, sh, &rows);
+    if (rows > p.slot_cap) bits |= ST_CAPACITY;
+    if (have) { s_start[s] = (int)min(r, (long long)p.slot_cap); p.row_start[s] = s_start[s]; }
+    if (threadIdx.x == 0) {
+      s_start[p.nseq] = (int)min(rows, (long long)p.slot_cap);
+      p.row_start[p.nseq] = s_start[p.nseq];
+    }
+    if (inline_slots) {
+      __threadfence_block();
+      __syncthreads();
+      for (int i = threadIdx.x; i < s_start[p.nseq]; i += PAGES_T) p.slot[i] = map_slot(p, s_start, i);
+    }
+  }
+  if (bits) set_status(p.status, bits);
+}
+
+__global__ void __launch_bounds__(256) slot_map_kernel(PageResizeParams p) {
+  __shared__ int starts[PAGES_MAX_SEQ + 1];
+  for (int i = threadIdx.x; i <= p.nseq; i += 256) starts[i] = p.row_start[i];
+  __syncthreads();
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < starts[p.nseq]) p.slot[r] = map_slot(p, starts, r);
+}
+
+hipError_t launch_page_resize(const PageResizeParams& p, hipStream_t st) {
+  const int inl = p.slot_cap <= PAGES_INLINE_ROWS;
+  hipLaunchKernelGGL(page_resize_kernel, dim3(1), dim3(PAGES_T), 0, st, p, inl);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.slot || inl) return e;
+  hipLaunchKernelGGL(slot_map_kernel, dim3((p.slot_cap + 255) / 256), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace dflow

@@ -63,6 +63,19 @@ class Sampler(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_float), ("seed", ctypes.c_uint64), ("stream", ctypes.c_void_p)]
 
 
+class KV8(ctypes.Structure):
+    """dflow_kv8: one layer's 8-bit cache."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("num_pages", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
+
+
+class Pool(ctypes.Structure):
+    """dflow_page_pool: page table rows and the free pages."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("max_pages", ctypes.c_int), ("n_held", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("num_pages", ctypes.c_int), ("n_free", ctypes.c_void_p)]
+
+
 EXPORTS = {
     "dflow_last_error": (ctypes.c_char_p, []),
     "dflow_packed_bytes": (ctypes.c_size_t, [ctypes.c_int, ctypes.c_int, ctypes.c_int]),
@@ -110,6 +123,18 @@ EXPORTS = {
     "dflow_bench_force_drafts": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
                                                 ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "dflow_page_resize": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(Pool), ctypes.c_int, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
+                                         ctypes.c_void_p]),
+    "dflow_kv8_append": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(KV8), ctypes.c_int,
+                                        ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t,
+                                        ctypes.c_void_p, ctypes.c_void_p]),
+    "dflow_kv8_attention_workspace": (ctypes.c_size_t, [ctypes.c_int] * 7),
+    "dflow_kv8_attention": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(KV8), ctypes.c_int,
+                                           ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_float, ctypes.c_int, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "dflow_read_status": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32),
                                          ctypes.c_int]),
     "dflow_profile": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int]),
