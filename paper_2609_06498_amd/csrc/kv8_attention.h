@@ -1,12 +1,14 @@
 // Attention over the paged 8-bit cache (included by attention.hip).
 //
 // o = sum_t softmax_t(scale q . k_t) v_t over the keys t a row sees, with
-// k_t = ks[t / 16] * code and v_t likewise.  A workgroup has TW x PW waves: wave
-// (tw, pw) owns RG groups of 16 rows (row = (token row j, query head g of the kv
-// head's group)) and every PW-th page of the split; the PW waves of a row tile
-// merge their running softmax states through LDS at the end.  K and V bytes go
-// from memory to registers without LDS, the next page's while this one is
-// worked on.
+// k_t = ks[t / 16] * code and v_t likewise.  Rows are (token row j, query head g of the
+// kv head's group) pairs, 16 to a row group.  Two kernels:
+//   one row group: four waves, each with every fourth page of the split; pages go from memory to registers, the next
+//     one's while this one is worked on;
+//   more rows: eight waves, TW row tiles x PW pages at a time; the pages go by
+//     load-to-LDS to a ring that the TW waves of a page share, each 16-byte run
+//     where its lane reads it; one barrier per page.
+// The PW states of a row tile are merged through LDS at the end.
 //
 // Per page a wave computes S^T = K Q^T (codes converted to bf16, exact; fp32
 // queries as three bf16 parts, so their 24 bits are all there) and O^T += V^T P^T
@@ -65,11 +67,10 @@ __device__ __forceinline__ uint32_t pk_f16(float a, float b) {   // round to nea
 
 // Work split of a launch, from the host's arguments only.
 struct Kv8Split {
-  int rg;                    // 16-row groups of a workgroup's row tile
-  int tiles;                 // row tiles of the longest sequence
+  int rg, tw, pw;            // 16-row groups of a wave, row tiles and pages of a workgroup's waves
+  int tiles;                 // workgroup tiles (rg tw row groups) of the longest sequence
   int split_pages, nsplit;
 };
-constexpr int KV8_WAVES = 4; // page waves of a workgroup
 
 // Rows of a sequence and the keys they see.
 struct Kv8Rows {
@@ -145,14 +146,14 @@ __device__ __forceinline__ uint32_t kv8_nan_bytes(uint32_t u) {
 // One running-softmax step of a 16-row group over a page: scores sc (key tile,
 // element) of the lane's 16 keys from key16 on, its key scale (times the softmax
 // scale, log2 units) c, log2 vs and 1 / vs; leaves the fp16 operands of P.
-template <int DT, int NP>
-__device__ __forceinline__ void kv8_softmax(const f32x4_t (&sc)[4], bool edge, int key16, int lim, float c, float ev,
+template <int DT, int NP, bool EDGE>
+__device__ __forceinline__ void kv8_softmax(const f32x4_t (&sc)[4], int key16, int lim, float c, float ev,
                                             float inv, float& M, float& l, f32x4_t (&o)[DT], u32x4_t (&pa)[2][NP]) {
   constexpr float HEAD = 8.f, SLACK = 7.f;
   float t[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) t[e] = sc[e >> 2][e & 3];
-  if (edge) {
+  if constexpr (EDGE) {
 #pragma unroll
     for (int e = 0; e < 16; ++e)
       if (key16 + e >= lim) t[e] = -INFINITY;
@@ -202,8 +203,8 @@ __device__ __forceinline__ void kv8_softmax(const f32x4_t (&sc)[4], bool edge, i
 
 // NaN values of an edge page: an output channel becomes NaN in the rows that see
 // such a key, found as a product of ones (a NaN; a key that the row sees).
-template <int DT, int RG>
-__device__ __forceinline__ void kv8_nan_values(const u32x4_t* vl, int key16, int lim_last, const int (&lim)[RG],
+template <int DT, int RG, typename V>
+__device__ __forceinline__ void kv8_nan_values(V&& vrun, int key16, int lim_last, const int (&lim)[RG],
                                                f32x4_t (&o)[RG][DT]) {
   constexpr uint32_t ONE8 = 0x38383838u, ONE16 = 0x3C00u;   // 1.0 as e4m3, as fp16
 #pragma unroll
@@ -218,7 +219,7 @@ __device__ __forceinline__ void kv8_nan_values(const u32x4_t* vl, int key16, int
       }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      u32x4_t u = kv8_clear_from(vl[d * 64], key16, lim_last);
+      u32x4_t u = kv8_clear_from(vrun(d), key16, lim_last);
 #pragma unroll
       for (int e = 0; e < 4; ++e) u[e] = kv8_nan_bytes(u[e]) & ONE8;
       f32x4_t n = mma_f16(kv8_f16(u[0], u[1]), sees[0], f32x4_t{0.f, 0.f, 0.f, 0.f});
@@ -230,12 +231,12 @@ __device__ __forceinline__ void kv8_nan_values(const u32x4_t* vl, int key16, int
   }
 }
 
-// Merges the states of the PW page waves, halves at a time, through LDS (kv8_smem,
-// (PW / 2) RG (DH / 4 + 2) 256 bytes; every wave is done with what it held), and
-// stores wave 0's: the output where the rows have one split, else a partial.
-template <typename T, int DH, int RG, int PW>
+// Merges the states of a row tile's PW page waves, halves at a time, through LDS
+// (TW (PW / 2) RG (DH / 4 + 2) 256 bytes; every wave is done with what it held), and
+// stores page wave 0's: the output where the rows have one split, else a partial.
+template <typename T, int DH, int RG, int TW, int PW>
 __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Split& sp, const Kv8Rows& rows, int s, int kvh,
-                                           int split, int nact, int R, int r0, int pw, float* smem, float (&M)[RG],
+                                           int split, int nact, int R, int r0, int tw, int pw, float* smem, float (&M)[RG],
                                            float (&l)[RG], f32x4_t (&o)[RG][DH / 16]) {
   constexpr int DT = DH / 16, REC = (DT * 4 + 2) * 64;   // floats of a row group's state, register by register
   const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
@@ -247,10 +248,10 @@ __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Spli
     pair32(a + b, a, b);
     l[x] = a + b;
   }
-  __syncthreads();
+  if constexpr (PW > 1) __syncthreads();
 #pragma unroll
   for (int half = PW / 2; half >= 1; half >>= 1) {
-    float* st = smem + (size_t)(pw % half) * RG * REC + lane;
+    float* st = smem + (size_t)(tw * (PW / 2) + pw % half) * RG * REC + lane;
     if (pw >= half && pw < 2 * half) {
 #pragma unroll
       for (int x = 0; x < RG; ++x) {
@@ -296,7 +297,7 @@ __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Spli
         kv8_store4<T>(p, rows.start + j, col + d * 16, y);
       }
     } else {
-      const size_t idx = (((size_t)s * Hkv + kvh) * sp.tiles * RG + r / 16) * sp.nsplit + split;
+      const size_t idx = (((size_t)s * Hkv + kvh) * sp.tiles * TW * RG + r / 16) * sp.nsplit + split;
       float* rec = p.part + idx * (16 * DH + 32);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
@@ -306,168 +307,286 @@ __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Spli
   }
 }
 
+// A wave's state, and one page against it: S^T = K Q^T, a softmax step, O^T += V^T P^T.
+template <typename T, int DH, int RG>
+struct Kv8Wave {
+  static constexpr int NQ = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
+  static constexpr int NP = sizeof(T) == 2 ? 1 : 2;  // fp16 parts of a probability
+  static constexpr int KI = DH / 64, KS = 2 * KI;    // 16-byte runs per key row and lane, k steps
+  static constexpr int DT = DH / 16;
+  u32x4_t qf[RG][KS][NQ];
+  int lim[RG], lim_last;                       // keys that lane % 16's row sees, that the wave's last row sees
+  float sl2;                                   // softmax scale, log2 units
+  float M[RG], l[RG];
+  f32x4_t o[RG][DT];                           // channel 16 dt + 4 g + r of row lane % 16
+
+  // rows from r0 on of the sequence's R (clamped rows are never stored)
+  __device__ __forceinline__ void load(const Kv8AttnParams& p, const Kv8Rows& rows, int kvh, int G, int r0, int R) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
+#pragma unroll
+    for (int i = 0; i < RG; ++i) {
+      const int r = min(r0 + i * 16 + m16, R - 1), j = r / G;
+      lim[i] = rows.limit(j, p.causal);
+      const T* q = reinterpret_cast<const T*>(p.q) + (size_t)(rows.start + j) * p.ld_q + (size_t)(kvh * G + r - j * G) * DH;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)             // k step 2 c + h: channels 64 c + 16 g + 8 h ..
+        kv8_query<T, NQ>(q + (k >> 1) * 64 + g * 16 + (k & 1) * 8, qf[i][k]);
+      M[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    lim_last = rows.limit((min(r0 + RG * 16, R) - 1) / G, p.causal);
+    sl2 = p.scale * 1.4426950408889634f;
+  }
+
+  // Page with first key kp0.  krun(kt, c), vrun(d): the lane's 16-byte runs; ksc,
+  // vsc: its group's scales; mid(): called between scores and softmax.  EDGE: some
+  // row sees a part of the page only, or (ok false: invalid page id) none does.
+  template <bool EDGE, typename K, typename V, typename F>
+  __device__ __forceinline__ void page(int kp0, bool ok, K&& krun, V&& vrun, float ksc, float vsc, F&& mid) {
+    const int key16 = kp0 + 16 * ((threadIdx.x & 63) >> 4);
+    f32x4_t sc[RG][4];
+#pragma unroll
+    for (int x = 0; x < RG; ++x)
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) sc[x][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int c = 0; c < KI; ++c) {
+        const u32x4_t u = krun(kt, c);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4_t kf = h ? kv8_bf16(u[2], u[3]) : kv8_bf16(u[0], u[1]);
+#pragma unroll
+          for (int x = 0; x < RG; ++x)
+#pragma unroll
+            for (int n = NQ - 1; n >= 0; --n) sc[x][kt] = mma_frag(bf16(), kf, qf[x][2 * c + h][n], sc[x][kt]);
+        }
+      }
+    int lm[RG], ll = lim_last;
+#pragma unroll
+    for (int x = 0; x < RG; ++x) lm[x] = lim[x];
+    if constexpr (EDGE) {
+      if (!ok) {                               // uniform
+        ll = 0;
+#pragma unroll
+        for (int x = 0; x < RG; ++x) lm[x] = 0;
+      }
+      if (key16 >= ll) ksc = vsc = 1.f;        // a group that no row sees may have any scale
+    }
+    const float c = sl2 * ksc, ev = __builtin_amdgcn_logf(vsc), inv = __builtin_amdgcn_rcpf(vsc);
+    mid();
+    u32x4_t pa[RG][2][NP];
+#pragma unroll
+    for (int x = 0; x < RG; ++x) kv8_softmax<DT, NP, EDGE>(sc[x], key16, lm[x], c, ev, inv, M[x], l[x], o[x], pa[x]);
+    uint32_t nan = 0;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      u32x4_t u = vrun(d);
+      if constexpr (EDGE) {                    // NaN would pass a zero probability: taken out here, and seen to below
+        u = kv8_clear_from(u, key16, ll);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t b = kv8_nan_bytes(u[e]);
+          nan |= b;
+          u[e] &= ~b;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4_t vf = h ? kv8_f16(u[2], u[3]) : kv8_f16(u[0], u[1]);
+#pragma unroll
+        for (int x = 0; x < RG; ++x)
+#pragma unroll
+          for (int n = NP - 1; n >= 0; --n) o[x][d] = mma_f16(vf, pa[x][h][n], o[x][d]);
+      }
+    }
+    if constexpr (EDGE)
+      if (__builtin_amdgcn_ballot_w64(nan != 0) != 0) kv8_nan_values<DT, RG>(vrun, key16, ll, lm, o);
+  }
+};
+
+// What a workgroup does: its rows and its pages.
+struct Kv8Item {
+  int s, kvh, split, tile, G, R, nact, p0, p1;
+  Kv8Rows rows;
+};
+// false: nothing to do (uniform).  pid0: a page id loaded for page p0 + first + step lane of the table row
+__device__ __forceinline__ bool kv8_item(const Kv8AttnParams& p, const Kv8Split& sp, int tile_rows, int first, int step,
+                                         Kv8Item& it, int& pid) {
+  const int Hkv = p.c.Hkv;
+  // kv head fastest (a page's heads are neighbours in memory), then split, row tile (last rows first), sequence
+  it.kvh = blockIdx.x % Hkv;
+  int rest = blockIdx.x / Hkv;
+  it.split = rest % sp.nsplit;
+  rest /= sp.nsplit;
+  it.tile = sp.tiles - 1 - rest % sp.tiles;
+  it.s = rest / sp.tiles;
+  it.p0 = it.split * sp.split_pages;
+  // (issued beside the lengths, which decide whether it counts)
+  pid = p.page_table[(size_t)it.s * p.max_pages + min(it.p0 + first + step * (int)(threadIdx.x & 63), p.max_pages - 1)];
+  it.G = p.Hq / Hkv;
+  int bits;
+  const bool ok = kv8_rows(p, it.s, it.rows, bits);
+  if (bits && it.tile == 0 && it.split == 0 && it.kvh == 0 && threadIdx.x == 0) set_status(p.status, bits);
+  it.R = ok ? it.rows.n * it.G : 0;
+  const int r0 = it.tile * tile_rows;
+  if (r0 >= it.R) return false;
+  const int lim = it.rows.limit((min(r0 + tile_rows, it.R) - 1) / it.G, p.causal);
+  it.nact = kv8_active(lim, sp.split_pages);
+  it.p1 = min(it.p0 + sp.split_pages, (lim + PAGE - 1) / PAGE);
+  return it.split < it.nact;
+}
+// invalid ids among the lane's np pages become -1 and set the status; whether there is one
+__device__ __forceinline__ bool kv8_check_ids(const Kv8AttnParams& p, int np, int& pid) {
+  const bool bad = (int)(threadIdx.x & 63) < np && (pid < 0 || pid >= p.c.num_pages);
+  if (bad) pid = -1;
+  const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
+  if (any && (threadIdx.x & 63) == 0) set_status(p.status, ST_BAD_PAGE);
+  return any;
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(256, 2) kv8_direct_kernel(Kv8AttnParams p, Kv8Split sp) {
+  constexpr int PW = 4, RG = 1;
+  typedef Kv8Wave<T, DH, RG> W;
+  extern __shared__ __align__(16) float kv8_smem[];
+  const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
+  const int pw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Kv8Item it;
+  int pid;
+  if (!kv8_item(p, sp, RG * 16, pw, PW, it, pid)) return;
+  const int Hkv = p.c.Hkv, r0 = it.tile * RG * 16, pbase = it.p0 + pw;
+  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // page pbase + PW i: id i in lane i (np <= 64)
+  const bool any_bad = kv8_check_ids(p, np, pid);
+  u32x4_t kr[4][W::KI], vr[W::DT];
+  float ksn, vsn;
+  const uint32_t koff = (16 * (m16 >> 2) + (m16 & 3)) * DH + g * 16, voff = m16 * 64 + g * 16;
+  auto head = [&](int i) { return (size_t)max(__builtin_amdgcn_readlane(pid, i), 0) * Hkv + it.kvh; };   // invalid: page 0, unused
+  auto issue_k = [&](int i) {
+    const size_t ph = head(i);
+    const uint8_t* kb = p.c.k + ph * PAGE * DH;
+    ksn = *(const gf32*)(p.c.ks + ph * 4 + g);
+    vsn = *(const gf32*)(p.c.vs + ph * 4 + g);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int c = 0; c < W::KI; ++c) kr[kt][c] = *(const gu4*)(kb + 4 * kt * DH + c * 64 + koff);
+  };
+  auto issue_v = [&](int i) {
+    const uint8_t* vb = p.c.v + head(i) * PAGE * DH;
+#pragma unroll
+    for (int d = 0; d < W::DT; ++d) vr[d] = *(const gu4*)(vb + d * 1024 + voff);
+  };
+  if (np > 0) {
+    issue_k(0);
+    issue_v(0);
+  }
+  W w;
+  w.load(p, it.rows, it.kvh, it.G, r0, it.R);
+  const int lim_first = it.rows.limit(r0 / it.G, p.causal);
+  auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
+    const int kp0 = (pbase + PW * i) * PAGE;
+    w.template page<EDGE>(
+        kp0, __builtin_amdgcn_readlane(pid, i) >= 0, [&](int kt, int c) { return kr[kt][c]; }, [&](int d) { return vr[d]; },
+        ksn, vsn, [&]() {
+          if (i + 1 < np) issue_k(i + 1);
+        });
+    if (i + 1 < np) issue_v(i + 1);
+  };
+  // whole pages first, then those that some row sees in part (all, if an id is invalid)
+  const int full = any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
+  int i = 0;
+  for (; i < full; ++i) step(i, std::integral_constant<bool, false>());
+  for (; i < np; ++i) step(i, std::integral_constant<bool, true>());
+  kv8_finish<T, DH, RG, 1, PW>(p, sp, it.rows, it.s, it.kvh, it.split, it.nact, it.R, r0, 0, pw, kv8_smem, w.M, w.l, w.o);
+}
+
 // 64 lanes x 4 bytes from base + voff to LDS bytes lds .. lds + 255
 __device__ __forceinline__ void load_to_lds4(uint32_t lds, const void* base, uint32_t voff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(base)
                : "memory", "m0");
 }
 
-template <typename T, int DH, int RG>
-__global__ void __launch_bounds__(256, 1) kv8_ring_kernel(Kv8AttnParams p, Kv8Split sp) {
-  constexpr int PW = 4;
-  constexpr int NQ = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
-  constexpr int NP = sizeof(T) == 2 ? 1 : 2;  // fp16 parts of a probability
-  constexpr int KI = DH / 64, KS = 2 * KI;    // 16-byte runs per key row and lane, k steps
-  constexpr int DT = DH / 16;
-  constexpr int NL = 4 * KI + DT + 2;         // loads of a page
-  constexpr uint32_t SLOT = (4 * KI + DT) * 1024 + 512;   // bytes of a ring slot: keys, values, scales
+// Ring slots of a page: as many as leave one workgroup of LDS, two at least.
+constexpr int kv8_slots(int pw) { return pw >= 4 ? 2 : 3; }
+template <int DH> constexpr uint32_t kv8_slot_bytes() { return DH / 8 * 1024 + 512; }   // keys, values, scales
+
+template <typename T, int DH, int RG, int TW>
+__global__ void __launch_bounds__(512, 2) kv8_shared_kernel(Kv8AttnParams p, Kv8Split sp) {
+  constexpr int PW = 8 / TW, NS = kv8_slots(PW);
+  typedef Kv8Wave<T, DH, RG> W;
+  constexpr int NR = 4 * W::KI + W::DT;       // 1 KB runs of a page: keys, then values
+  constexpr int LPW = NR / TW + 2;            // loads of a wave and page (the scales by every wave)
+  constexpr uint32_t SLOT = kv8_slot_bytes<DH>();
+  static_assert(NR % TW == 0 && SLOT == NR * 1024 + 512, "runs split evenly over the tile waves");
   extern __shared__ __align__(16) float kv8_smem[];
   const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
-  const int pw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int Hkv = p.c.Hkv, G = p.Hq / Hkv;
-  // kv head fastest (a page's heads are neighbours in memory), then split, row tile (last rows first), sequence
-  const int kvh = blockIdx.x % Hkv;
-  int rest = blockIdx.x / Hkv;
-  const int split = rest % sp.nsplit;
-  rest /= sp.nsplit;
-  const int tile = sp.tiles - 1 - rest % sp.tiles, s = rest / sp.tiles;
-  Kv8Rows rows;
-  int bits;
-  const bool ok_rows = kv8_rows(p, s, rows, bits);
-  if (bits && tile == 0 && split == 0 && kvh == 0 && threadIdx.x == 0) set_status(p.status, bits);
-  const int R = ok_rows ? rows.n * G : 0, r0 = tile * RG * 16;
-  if (r0 >= R) return;                         // uniform over the workgroup
-  const int lim_first = rows.limit(r0 / G, p.causal);
-  const int lim_last = rows.limit((min(r0 + RG * 16, R) - 1) / G, p.causal);
-  const int nact = kv8_active(lim_last, sp.split_pages);
-  if (split >= nact) return;
-  const int p0 = split * sp.split_pages, p1 = min(p0 + sp.split_pages, (lim_last + PAGE - 1) / PAGE);
-
-  // the wave's pages: p0 + pw + PW i, page id i in lane i (split_pages <= 64 PW)
-  const int np = p1 > p0 + pw ? (p1 - p0 - pw + PW - 1) / PW : 0;
-  int pid = 0;
-  if (np > 0) pid = p.page_table[(size_t)s * p.max_pages + min(p0 + pw + PW * min(lane, np - 1), p.max_pages - 1)];
-  const bool bad = np > 0 && (pid < 0 || pid >= p.c.num_pages);
-  if (__builtin_amdgcn_ballot_w64(bad) != 0 && lane == 0) set_status(p.status, ST_BAD_PAGE);
-  if (bad) pid = -1;
-
-  int lim[RG];                                 // of lane % 16's row (clamped rows are never stored)
-  u32x4_t qf[RG][KS][NQ];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int pw = wv % PW, tw = wv / PW;
+  Kv8Item it;
+  int pid;
+  if (!kv8_item(p, sp, TW * RG * 16, pw, PW, it, pid)) return;
+  const int Hkv = p.c.Hkv, r0 = (it.tile * TW + tw) * RG * 16, pbase = it.p0 + pw;
+  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // page pbase + PW i: id i in lane i (np <= 64)
+  const int steps = it.p1 > it.p0 ? (it.p1 - it.p0 + PW - 1) / PW : 0;   // of the workgroup
+  const bool any_bad = kv8_check_ids(p, np, pid);
+  unsigned char* ring = reinterpret_cast<unsigned char*>(kv8_smem) + pw * NS * SLOT;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kv8_smem + pw * NS * SLOT;
+  const uint32_t koff = (16 * (m16 >> 2) + (m16 & 3)) * DH + g * 16, voff = m16 * 64 + g * 16, soff = g * 4;
+  W w;
+  const bool own = r0 < it.R;                  // uniform: the wave has rows (else it only helps to load)
+  w.load(p, it.rows, it.kvh, it.G, r0, it.R);
+  const int lim_first = it.rows.limit(min(r0, it.R - 1) / it.G, p.causal);
 #pragma unroll
-  for (int i = 0; i < RG; ++i) {
-    const int r = min(r0 + i * 16 + m16, R - 1), j = r / G;
-    lim[i] = rows.limit(j, p.causal);
-    const T* q = reinterpret_cast<const T*>(p.q) + (size_t)(rows.start + j) * p.ld_q + (size_t)(kvh * G + r - j * G) * DH;
+  for (int x = 0; x < RG; ++x)
 #pragma unroll
-    for (int k = 0; k < KS; ++k)               // k step 2 c + h: channels 64 c + 16 g + 8 h ..
-      kv8_query<T, NQ>(q + (k >> 1) * 64 + g * 16 + (k & 1) * 8, qf[i][k]);
-  }
-#pragma unroll
-  for (int i = 0; i < RG; ++i)
-#pragma unroll
-    for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(qf[i][k][0]));   // the rows are in before the ring's loads are counted
-
-  // the wave's ring of two pages, each fragment where its lane reads it
-  unsigned char* ring = reinterpret_cast<unsigned char*>(kv8_smem) + pw * 2 * SLOT;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kv8_smem + pw * 2 * SLOT;
-  const uint32_t koff = (16 * (m16 >> 2) + (m16 & 3)) * DH + g * 16, voff = lane / 16 * 16 + m16 * 64, soff = g * 4;
-  auto issue = [&](int i) {
-    const size_t ph = (size_t)max(__builtin_amdgcn_readlane(pid, i), 0) * Hkv + kvh;   // an invalid id reads page 0, unused
-    const uint32_t l = lds0 + (i & 1) * SLOT;
+    for (int k = 0; k < W::KS; ++k) asm volatile("" ::"v"(w.qf[x][k][0]));   // the rows are in before the ring's loads are counted
+  auto issue = [&](int i, uint32_t slot) {     // the wave's part of page i
+    const size_t ph = (size_t)max(__builtin_amdgcn_readlane(pid, i), 0) * Hkv + it.kvh;   // invalid: page 0, unused
+    const uint32_t l = lds0 + slot * SLOT;
     const uint8_t* kb = p.c.k + ph * PAGE * DH;
     const uint8_t* vb = p.c.v + ph * PAGE * DH;
-    load_to_lds4(l + (4 * KI + DT) * 1024, p.c.ks + ph * 4, soff);
-    load_to_lds4(l + (4 * KI + DT) * 1024 + 256, p.c.vs + ph * 4, soff);
-    static_for<4 * KI>([&]<int N>(std::integral_constant<int, N>) {
-      load_to_lds<N * 1024>(l, kb + (N / KI) * 4 * DH + (N % KI) * 64, koff);
-    });
-    static_for<DT>([&]<int N>(std::integral_constant<int, N>) {
-      load_to_lds<(4 * KI + N) * 1024>(l, vb + N * 1024, voff);
+    load_to_lds4(l + NR * 1024, p.c.ks + ph * 4, soff);
+    load_to_lds4(l + NR * 1024 + 256, p.c.vs + ph * 4, soff);
+    static_for<NR / TW>([&]<int N>(std::integral_constant<int, N>) {
+      const int n = tw * (NR / TW) + N;        // uniform
+      if (n < 4 * W::KI) load_to_lds<0>(l + n * 1024, kb + (n / W::KI) * 4 * DH + (n % W::KI) * 64, koff);
+      else load_to_lds<0>(l + n * 1024, vb + (n - 4 * W::KI) * 1024, voff);
     });
   };
-
-  const float sl2 = p.scale * 1.4426950408889634f;
-  float M[RG], l[RG];
-  f32x4_t o[RG][DT];                           // channel 16 dt + 4 g + r of row lane % 16
-#pragma unroll
-  for (int i = 0; i < RG; ++i) {
-    M[i] = -INFINITY;
-    l[i] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < NS - 1 && i < np; ++i) issue(i, i);
+  int slot = 0;
+  // Page i is in (its loads waited for by every wave that issued a part) and page i - 1 read by all: its slot takes page i + NS - 1.
+  auto begin = [&](int i) {
+    if (i + NS - 1 <= np) wait_barrier<(NS - 2) * LPW>();
+    else wait_barrier<0>();
+    if (i + NS - 1 < np) issue(i + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+  };
+  auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
+    const unsigned char* sb = ring + slot * SLOT;
+    const u32x4_t* runs = reinterpret_cast<const u32x4_t*>(sb) + lane;
+    const float* scl = reinterpret_cast<const float*>(sb + NR * 1024) + lane;
+    w.template page<EDGE>(
+        (pbase + PW * i) * PAGE, __builtin_amdgcn_readlane(pid, i) >= 0,
+        [&](int kt, int c) { return runs[(kt * W::KI + c) * 64]; }, [&](int d) { return runs[(4 * W::KI + d) * 64]; },
+        scl[0], scl[64], []() {});
+  };
+  auto next = [&]() { slot = slot + 1 == NS ? 0 : slot + 1; };
+  // whole pages first, then those that some row sees in part (all, if an id is invalid)
+  const int full = !own || any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
+  int i = 0;
+  for (; i < full; ++i, next()) {
+    begin(i);
+    step(i, std::integral_constant<bool, false>());
   }
-  if (np > 0) issue(0);
-  if (np > 1) issue(1);
-  for (int i = 0; i < np; ++i) {
-    if (i + 1 < np) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const unsigned char* slot = ring + (i & 1) * SLOT;
-    const u32x4_t* kl = reinterpret_cast<const u32x4_t*>(slot) + lane;
-    const u32x4_t* vl = reinterpret_cast<const u32x4_t*>(slot + 4 * KI * 1024) + lane;
-    const float* scl = reinterpret_cast<const float*>(slot + (4 * KI + DT) * 1024) + lane;
-    const int kp0 = (p0 + pw + PW * i) * PAGE;
-    if (__builtin_amdgcn_readlane(pid, i) >= 0) {             // uniform
-      const bool edge = kp0 + PAGE > lim_first;               // uniform: some row sees a part only
-      f32x4_t sc[RG][4];
-#pragma unroll
-      for (int x = 0; x < RG; ++x)
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) sc[x][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int c = 0; c < KI; ++c) {
-          const u32x4_t u = kl[(kt * KI + c) * 64];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x4_t kf = h ? kv8_bf16(u[2], u[3]) : kv8_bf16(u[0], u[1]);
-#pragma unroll
-            for (int x = 0; x < RG; ++x)
-#pragma unroll
-              for (int n = NQ - 1; n >= 0; --n) sc[x][kt] = mma_frag(bf16(), kf, qf[x][2 * c + h][n], sc[x][kt]);
-          }
-        }
-      // a group that no row sees may have any scale
-      const bool seen = kp0 + 16 * g < lim_last;
-      const float ksc = seen ? scl[0] : 1.f, vsc = seen ? scl[64] : 1.f;
-      const float c = sl2 * ksc, ev = __builtin_amdgcn_logf(vsc), inv = 1.f / vsc;
-      u32x4_t pa[RG][2][NP];
-#pragma unroll
-      for (int x = 0; x < RG; ++x) {
-        __builtin_amdgcn_sched_barrier(0);
-        kv8_softmax<DT, NP>(sc[x], edge, kp0 + 16 * g, lim[x], c, ev, inv, M[x], l[x], o[x], pa[x]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      uint32_t nan = 0;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        u32x4_t u = vl[d * 64];
-        if (edge) {                            // NaN would pass a zero probability: taken out here, and seen to below
-          u = kv8_clear_from(u, kp0 + 16 * g, lim_last);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t b = kv8_nan_bytes(u[e]);
-            nan |= b;
-            u[e] &= ~b;
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4_t vf = h ? kv8_f16(u[2], u[3]) : kv8_f16(u[0], u[1]);
-#pragma unroll
-          for (int x = 0; x < RG; ++x)
-#pragma unroll
-            for (int n = NP - 1; n >= 0; --n) o[x][d] = mma_f16(vf, pa[x][h][n], o[x][d]);
-        }
-      }
-      if (__builtin_amdgcn_ballot_w64(nan != 0) != 0) kv8_nan_values<DT, RG>(vl, kp0 + 16 * g, lim_last, lim, o);
-    }
-    if (i + 2 < np) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot is read
-      issue(i + 2);
-    }
+  for (; i < steps; ++i, next()) {
+    begin(i);
+    if (own && i < np && (pbase + PW * i) * PAGE < w.lim_last) step(i, std::integral_constant<bool, true>());   // uniform
   }
-  kv8_finish<T, DH, RG, PW>(p, sp, rows, s, kvh, split, nact, R, r0, pw, kv8_smem, M, l, o);
+  kv8_finish<T, DH, RG, TW, PW>(p, sp, it.rows, it.s, it.kvh, it.split, it.nact, it.R, r0, tw, pw, kv8_smem, w.M, w.l, w.o);
 }
 
 // Merges the splits of one 16-row group in split order: wave d the 16 channels
@@ -475,32 +594,44 @@ __global__ void __launch_bounds__(256, 1) kv8_ring_kernel(Kv8AttnParams p, Kv8Sp
 template <typename T, int DH>
 __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams p, Kv8Split sp) {
   const int lane = threadIdx.x & 63, d = threadIdx.x >> 6;
-  const int Hkv = p.c.Hkv, G = p.Hq / Hkv, rgs = sp.tiles * sp.rg;
+  const int Hkv = p.c.Hkv, G = p.Hq / Hkv, tile_rg = sp.tw * sp.rg, rgs = sp.tiles * tile_rg;
   const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, rg = rest % rgs, s = rest / rgs;
   Kv8Rows rows;
   int bits;
   if (!kv8_rows(p, s, rows, bits)) return;
   const int R = rows.n * G;
   if (rg * 16 >= R) return;
-  const int tile_end = min((rg / sp.rg + 1) * sp.rg * 16, R);
+  const int tile_end = min((rg / tile_rg + 1) * tile_rg * 16, R);
   const int nact = kv8_active(rows.limit((tile_end - 1) / G, p.causal), sp.split_pages);
   if (nact == 1) return;
   const float* rec = p.part + (((size_t)s * Hkv + kvh) * rgs + rg) * sp.nsplit * (16 * DH + 32);
   const int r = rg * 16 + (lane & 15);
+  constexpr int REC = 16 * DH + 32, U = 8;
+  const float* pv = rec + (d * 64 + lane) * 4;
+  const float* pm = rec + 16 * DH + 2 * (lane & 15);
   float M = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < nact; ++i) {
-    const float* ml = rec + (size_t)i * (16 * DH + 32) + 16 * DH + 2 * (lane & 15);
-    const float mi = ml[0], li = ml[1];
-    const float4 v = *reinterpret_cast<const float4*>(rec + (size_t)i * (16 * DH + 32) + (d * 64 + lane) * 4);
-    const float mn = fmaxf(M, mi);
-    const float f1 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-    const float f2 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mn);
-    l = l * f1 + li * f2;
-    y[0] = y[0] * f1 + v.x * f2;
-    y[1] = y[1] * f1 + v.y * f2;
-    y[2] = y[2] * f1 + v.z * f2;
-    y[3] = y[3] * f1 + v.w * f2;
-    M = mn;
+  for (int i = 0; i < nact; i += U) {          // U splits' loads in flight together (past the last: it again, unused)
+    float2 ml[U];
+    float4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (size_t)min(i + u, nact - 1) * REC;
+      ml[u] = *reinterpret_cast<const float2*>(pm + at);
+      v[u] = *reinterpret_cast<const float4*>(pv + at);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float mi = i + u < nact ? ml[u].x : -INFINITY;
+      const float mn = fmaxf(M, mi);
+      const float f1 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+      const float f2 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mn);
+      l = l * f1 + (f2 == 0.f ? 0.f : ml[u].y * f2);
+      y[0] = y[0] * f1 + (f2 == 0.f ? 0.f : v[u].x * f2);
+      y[1] = y[1] * f1 + (f2 == 0.f ? 0.f : v[u].y * f2);
+      y[2] = y[2] * f1 + (f2 == 0.f ? 0.f : v[u].z * f2);
+      y[3] = y[3] * f1 + (f2 == 0.f ? 0.f : v[u].w * f2);
+      M = mn;
+    }
   }
   if (r >= R) return;
 #pragma unroll
@@ -509,56 +640,73 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
   kv8_store4<T>(p, rows.start + j, (kvh * G + r - j * G) * DH + d * 16 + 4 * (lane >> 4), y);
 }
 
-// Work split: 16 rows a wave up to 16 rows per kv head, 32 beyond (bf16: the
-// converted keys and values serve two row groups), and of a workgroup's waves as
-// many on row tiles as the rows fill, the others on pages.  Pages per split: so
-// that the launch has about two workgroups per compute unit if every sequence
-// reaches key_cap, at least one page per page wave.  A function of the host's
-// arguments only.
+// Work split, a function of the host's arguments only.  One row group: the direct
+// kernel; more: as many row tiles of a workgroup's eight waves as the rows fill,
+// the other waves on pages.  Pages per split: so that
+// the launch has about two workgroups per compute unit if every sequence reaches
+// key_cap, at least one page per page wave, at most 64 (a page id per lane).
 inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int cus) {
   const long long R = (long long)max_rows * (Hq / Hkv);
   Kv8Split sp;
-  sp.rg = !bf16 || R <= 16 ? 1 : (R <= 32 ? 2 : 4);
-  sp.tiles = (int)((R + 16 * sp.rg - 1) / (16 * sp.rg));
+  sp.rg = bf16 && R > 32 ? 2 : 1;
+  const int per = 16 * sp.rg;
+  sp.tw = R <= per ? 1 : (R <= 2 * per ? 2 : (R <= 4 * per ? 4 : 8));
+  sp.pw = sp.tw == 1 ? 4 : 8 / sp.tw;
+  sp.tiles = (int)((R + per * sp.tw - 1) / (per * sp.tw));
   const long long items = (long long)nseq * Hkv * sp.tiles;
   const int pages = key_cap > 0 ? (key_cap + PAGE - 1) / PAGE : 1;
   const long long want = items < 2 * cus ? 2 * cus / items : 1;
   long long pp = (pages + want - 1) / want;
-  if (pp < KV8_WAVES) pp = KV8_WAVES;
-  if (pp > 64 * KV8_WAVES) pp = 64 * KV8_WAVES;
+  if (pp < sp.pw) pp = sp.pw;
+  if (pp > 64 * sp.pw) pp = 64 * sp.pw;
   sp.split_pages = (int)pp;
   sp.nsplit = (int)((pages + pp - 1) / pp);
   return sp;
 }
 
 inline size_t kv8_part_floats(const Kv8Split& sp, int nseq, int Hkv, int Dh) {
-  return sp.nsplit == 1 ? 0 : (size_t)nseq * Hkv * sp.tiles * sp.rg * sp.nsplit * (16 * Dh + 32);
+  return sp.nsplit == 1 ? 0 : (size_t)nseq * Hkv * sp.tiles * sp.tw * sp.rg * sp.nsplit * (16 * Dh + 32);
 }
 
-template <typename T, int DH, int RG>
-static hipError_t launch_kv8_shape(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
-  constexpr size_t ring = KV8_WAVES * 2 * (size_t)(DH / 8 * 1024 + 512);
-  constexpr size_t merge = (size_t)(KV8_WAVES / 2) * RG * (DH / 4 + 2) * 64 * sizeof(float);
-  constexpr size_t lds = ring > merge ? ring : merge;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_ring_kernel<T, DH, RG>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+template <auto KERNEL>
+static hipError_t launch_kv8_kernel(const Kv8AttnParams& p, const Kv8Split& sp, int threads, size_t lds, hipStream_t st) {
+  static const hipError_t attr =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr != hipSuccess) return attr;
   const long long wgs = (long long)p.nseq * p.c.Hkv * sp.tiles * sp.nsplit;
   if (wgs > 0x7FFFFFFFll) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((kv8_ring_kernel<T, DH, RG>), dim3((unsigned)wgs), dim3(KV8_WAVES * 64), lds, st, p, sp);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sp.nsplit == 1) return e;
-  hipLaunchKernelGGL((kv8_combine_kernel<T, DH>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.rg), dim3(DH * 4), 0, st, p, sp);
+  hipLaunchKernelGGL(KERNEL, dim3((unsigned)wgs), dim3(threads), lds, st, p, sp);
   return hipGetLastError();
+}
+
+constexpr size_t kv8_merge_bytes(int DH, int RG, int TW, int PW) {
+  return (size_t)TW * (PW / 2) * RG * (DH / 4 + 2) * 64 * sizeof(float);
+}
+
+template <typename T, int DH>
+static hipError_t launch_kv8_direct(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
+  return launch_kv8_kernel<&kv8_direct_kernel<T, DH>>(p, sp, 256, kv8_merge_bytes(DH, 1, 1, 4), st);
+}
+template <typename T, int DH, int RG, int TW>
+static hipError_t launch_kv8_shared(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
+  constexpr size_t ring = (size_t)(8 / TW) * kv8_slots(8 / TW) * kv8_slot_bytes<DH>();
+  constexpr size_t merge = kv8_merge_bytes(DH, RG, TW, 8 / TW);
+  return launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, 512, ring > merge ? ring : merge, st);
 }
 
 template <typename T, int DH>
 static hipError_t launch_kv8_dh(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if (sp.rg == 4) return launch_kv8_shape<T, DH, 4>(p, sp, st);
-    if (sp.rg == 2) return launch_kv8_shape<T, DH, 2>(p, sp, st);
-  }
-  return launch_kv8_shape<T, DH, 1>(p, sp, st);
+  constexpr int RG = sizeof(T) == 2 ? 2 : 1;
+  hipError_t e;
+  if (sp.tw == 8) e = launch_kv8_shared<T, DH, RG, 8>(p, sp, st);
+  else if (sp.tw == 4) e = launch_kv8_shared<T, DH, RG, 4>(p, sp, st);
+  else if (sp.tw == 2 && sp.rg == RG) e = launch_kv8_shared<T, DH, RG, 2>(p, sp, st);
+  else if (sp.tw == 2) e = launch_kv8_shared<T, DH, 1, 2>(p, sp, st);
+  else e = launch_kv8_direct<T, DH>(p, sp, st);
+  if (e != hipSuccess || sp.nsplit == 1) return e;
+  hipLaunchKernelGGL((kv8_combine_kernel<T, DH>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.tw * sp.rg), dim3(DH * 4), 0, st,
+                     p, sp);
+  return hipGetLastError();
 }
 
 size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus) {
