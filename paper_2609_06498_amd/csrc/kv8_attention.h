@@ -351,11 +351,18 @@ struct Kv8Wave {
     for (int x = 0; x < RG; ++x)
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) sc[x][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // all of a page's runs are asked for ahead of their use: the keys at once, the values under the softmax
+    u32x4_t kk[4][KI], vv[DT];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int c = 0; c < KI; ++c) kk[kt][c] = krun(kt, c);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
       for (int c = 0; c < KI; ++c) {
-        const u32x4_t u = krun(kt, c);
+        const u32x4_t u = kk[kt][c];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const u32x4_t kf = h ? kv8_bf16(u[2], u[3]) : kv8_bf16(u[0], u[1]);
@@ -378,13 +385,16 @@ struct Kv8Wave {
     }
     const float c = sl2 * ksc, ev = __builtin_amdgcn_logf(vsc), inv = __builtin_amdgcn_rcpf(vsc);
     mid();
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vv[d] = vrun(d);
+    __builtin_amdgcn_sched_barrier(0);
     u32x4_t pa[RG][2][NP];
 #pragma unroll
     for (int x = 0; x < RG; ++x) kv8_softmax<DT, NP, EDGE>(sc[x], key16, lm[x], c, ev, inv, M[x], l[x], o[x], pa[x]);
     uint32_t nan = 0;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      u32x4_t u = vrun(d);
+      u32x4_t u = vv[d];
       if constexpr (EDGE) {                    // NaN would pass a zero probability: taken out here, and seen to below
         u = kv8_clear_from(u, key16, ll);
 #pragma unroll
