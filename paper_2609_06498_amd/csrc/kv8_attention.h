@@ -5,7 +5,7 @@
 // kv head's group) pairs, 16 to a row group.  Two kernels:
 //   one row group: four waves, each with every fourth page of the split; pages go from memory to registers, the next
 //     one's while this one is worked on;
-//   more rows: eight waves, TW row tiles x PW pages at a time; the pages go by
+//   more rows: four waves, TW row tiles x PW pages at a time; the pages go by
 //     load-to-LDS to a ring that the TW waves of a page share, each 16-byte run
 //     where its lane reads it; one barrier per page.
 // The PW states of a row tile are merged through LDS at the end.
@@ -340,24 +340,18 @@ struct Kv8Wave {
     sl2 = p.scale * 1.4426950408889634f;
   }
 
-  // Page with first key kp0.  krun(kt, c), vrun(d): the lane's 16-byte runs; ksc,
-  // vsc: its group's scales; mid(): called between scores and softmax.  EDGE: some
-  // row sees a part of the page only, or (ok false: invalid page id) none does.
-  template <bool EDGE, typename K, typename V, typename F>
-  __device__ __forceinline__ void page(int kp0, bool ok, K&& krun, V&& vrun, float ksc, float vsc, F&& mid) {
+  // Page with first key kp0.  kk, vrun(d): the lane's 16-byte runs; ksc, vsc: its
+  // group's scales; mid(): called when kk and the scales are used up, to refill
+  // them for the next page.  EDGE: some row sees a part of the page only, or (ok
+  // false: invalid page id) none does.
+  template <bool EDGE, typename V, typename F>
+  __device__ __forceinline__ void page(int kp0, bool ok, u32x4_t (&kk)[4][KI], V&& vrun, float ksc, float vsc, F&& mid) {
     const int key16 = kp0 + 16 * ((threadIdx.x & 63) >> 4);
     f32x4_t sc[RG][4];
 #pragma unroll
     for (int x = 0; x < RG; ++x)
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) sc[x][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // all of a page's runs are asked for ahead of their use: the keys at once, the values under the softmax
-    u32x4_t kk[4][KI], vv[DT];
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-      for (int c = 0; c < KI; ++c) kk[kt][c] = krun(kt, c);
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
@@ -384,9 +378,10 @@ struct Kv8Wave {
       if (key16 >= ll) ksc = vsc = 1.f;        // a group that no row sees may have any scale
     }
     const float c = sl2 * ksc, ev = __builtin_amdgcn_logf(vsc), inv = __builtin_amdgcn_rcpf(vsc);
-    mid();
+    u32x4_t vv[DT];                            // asked for ahead of their use, under the softmax
 #pragma unroll
     for (int d = 0; d < DT; ++d) vv[d] = vrun(d);
+    mid();
     __builtin_amdgcn_sched_barrier(0);
     u32x4_t pa[RG][2][NP];
 #pragma unroll
@@ -500,8 +495,7 @@ __global__ void __launch_bounds__(256, 2) kv8_direct_kernel(Kv8AttnParams p, Kv8
   auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
     const int kp0 = (pbase + PW * i) * PAGE;
     w.template page<EDGE>(
-        kp0, __builtin_amdgcn_readlane(pid, i) >= 0, [&](int kt, int c) { return kr[kt][c]; }, [&](int d) { return vr[d]; },
-        ksn, vsn, [&]() {
+        kp0, __builtin_amdgcn_readlane(pid, i) >= 0, kr, [&](int d) { return vr[d]; }, ksn, vsn, [&]() {
           if (i + 1 < np) issue_k(i + 1);
         });
     if (i + 1 < np) issue_v(i + 1);
@@ -520,13 +514,20 @@ __device__ __forceinline__ void load_to_lds4(uint32_t lds, const void* base, uin
                : "memory", "m0");
 }
 
-// Ring slots of a page: as many as leave one workgroup of LDS, two at least.
-constexpr int kv8_slots(int pw) { return pw >= 4 ? 2 : 3; }
+// Four waves and up to 80 KB of LDS, so that two workgroups, at no fixed distance
+// from each other, share a compute unit: one's matrix operations run beside the
+// other's softmax.
+// Ring slots of a page: with one page at a time four, and the next page's keys
+// are read ahead; with two pages two.
+constexpr int KV8_SHARED_WAVES = 4;
+constexpr int kv8_slots(int pw) { return pw == 1 ? 4 : 2; }
 template <int DH> constexpr uint32_t kv8_slot_bytes() { return DH / 8 * 1024 + 512; }   // keys, values, scales
 
 template <typename T, int DH, int RG, int TW>
-__global__ void __launch_bounds__(512, 2) kv8_shared_kernel(Kv8AttnParams p, Kv8Split sp) {
-  constexpr int PW = 8 / TW, NS = kv8_slots(PW);
+__global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv8AttnParams p, Kv8Split sp) {
+  constexpr int PW = KV8_SHARED_WAVES / TW, NS = kv8_slots(PW);
+  constexpr int AHEAD = PW == 1 ? 1 : 0;      // pages that are in beyond the present one
+  static_assert(NS >= AHEAD + 2, "a slot to load while the resident ones are read");
   typedef Kv8Wave<T, DH, RG> W;
   constexpr int NR = 4 * W::KI + W::DT;       // 1 KB runs of a page: keys, then values
   constexpr int LPW = NR / TW + 2;            // loads of a wave and page (the scales by every wave)
@@ -569,25 +570,46 @@ __global__ void __launch_bounds__(512, 2) kv8_shared_kernel(Kv8AttnParams p, Kv8
   };
   for (int i = 0; i < NS - 1 && i < np; ++i) issue(i, i);
   int slot = 0;
-  // Page i is in (its loads waited for by every wave that issued a part) and page i - 1 read by all: its slot takes page i + NS - 1.
+  // Page i + AHEAD is in (its loads waited for by every wave that issued a part) and page i - 1 read by all: its slot
+  // takes page i + NS - 1.
   auto begin = [&](int i) {
-    if (i + NS - 1 <= np) wait_barrier<(NS - 2) * LPW>();
+    if (i + NS - 1 <= np) wait_barrier<(NS - 2 - AHEAD) * LPW>();
     else wait_barrier<0>();
     if (i + NS - 1 < np) issue(i + NS - 1, slot == 0 ? NS - 1 : slot - 1);
   };
-  auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
-    const unsigned char* sb = ring + slot * SLOT;
+  u32x4_t kk[4][W::KI];
+  float ksc, vsc;
+  auto read_keys = [&](int sl) {
+    const unsigned char* sb = ring + sl * SLOT;
     const u32x4_t* runs = reinterpret_cast<const u32x4_t*>(sb) + lane;
     const float* scl = reinterpret_cast<const float*>(sb + NR * 1024) + lane;
-    w.template page<EDGE>(
-        (pbase + PW * i) * PAGE, __builtin_amdgcn_readlane(pid, i) >= 0,
-        [&](int kt, int c) { return runs[(kt * W::KI + c) * 64]; }, [&](int d) { return runs[(4 * W::KI + d) * 64]; },
-        scl[0], scl[64], []() {});
+    ksc = scl[0];
+    vsc = scl[64];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int c = 0; c < W::KI; ++c) kk[kt][c] = runs[(kt * W::KI + c) * 64];
+  };
+  auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
+    const u32x4_t* runs = reinterpret_cast<const u32x4_t*>(ring + slot * SLOT) + lane;
+    if constexpr (!AHEAD) {
+      read_keys(slot);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    w.template page<EDGE>((pbase + PW * i) * PAGE, __builtin_amdgcn_readlane(pid, i) >= 0, kk,
+                          [&](int d) { return runs[(4 * W::KI + d) * 64]; }, ksc, vsc, [&]() {
+                            if constexpr (AHEAD) read_keys(slot + 1 == NS ? 0 : slot + 1);   // (past the last page: unused)
+                          });
   };
   auto next = [&]() { slot = slot + 1 == NS ? 0 : slot + 1; };
   // whole pages first, then those that some row sees in part (all, if an id is invalid)
   const int full = !own || any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
   int i = 0;
+  if (AHEAD && steps > 0) {
+    if (np >= NS - 1) wait_barrier<(NS - 2) * LPW>();
+    else wait_barrier<0>();
+    read_keys(0);
+  }
   for (; i < full; ++i, next()) {
     begin(i);
     step(i, std::integral_constant<bool, false>());
@@ -651,7 +673,7 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
 }
 
 // Work split, a function of the host's arguments only.  One row group: the direct
-// kernel; more: as many row tiles of a workgroup's eight waves as the rows fill,
+// kernel; more: as many row tiles of a workgroup's four waves as the rows fill,
 // the other waves on pages.  Pages per split: so that
 // the launch has about two workgroups per compute unit if every sequence reaches
 // key_cap, at least one page per page wave, at most 64 (a page id per lane).
@@ -660,8 +682,8 @@ inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq
   Kv8Split sp;
   sp.rg = bf16 && R > 32 ? 2 : 1;
   const int per = 16 * sp.rg;
-  sp.tw = R <= per ? 1 : (R <= 2 * per ? 2 : (R <= 4 * per ? 4 : 8));
-  sp.pw = sp.tw == 1 ? 4 : 8 / sp.tw;
+  sp.tw = R <= per ? 1 : (R <= 2 * per ? 2 : 4);
+  sp.pw = 4 / sp.tw;
   sp.tiles = (int)((R + per * sp.tw - 1) / (per * sp.tw));
   const long long items = (long long)nseq * Hkv * sp.tiles;
   const int pages = key_cap > 0 ? (key_cap + PAGE - 1) / PAGE : 1;
@@ -699,17 +721,17 @@ static hipError_t launch_kv8_direct(const Kv8AttnParams& p, const Kv8Split& sp, 
 }
 template <typename T, int DH, int RG, int TW>
 static hipError_t launch_kv8_shared(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
-  constexpr size_t ring = (size_t)(8 / TW) * kv8_slots(8 / TW) * kv8_slot_bytes<DH>();
-  constexpr size_t merge = kv8_merge_bytes(DH, RG, TW, 8 / TW);
-  return launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, 512, ring > merge ? ring : merge, st);
+  constexpr int PW = KV8_SHARED_WAVES / TW;
+  constexpr size_t ring = (size_t)PW * kv8_slots(PW) * kv8_slot_bytes<DH>();
+  constexpr size_t merge = kv8_merge_bytes(DH, RG, TW, PW);
+  return launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, KV8_SHARED_WAVES * 64, ring > merge ? ring : merge, st);
 }
 
 template <typename T, int DH>
 static hipError_t launch_kv8_dh(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
   constexpr int RG = sizeof(T) == 2 ? 2 : 1;
   hipError_t e;
-  if (sp.tw == 8) e = launch_kv8_shared<T, DH, RG, 8>(p, sp, st);
-  else if (sp.tw == 4) e = launch_kv8_shared<T, DH, RG, 4>(p, sp, st);
+  if (sp.tw == 4) e = launch_kv8_shared<T, DH, RG, 4>(p, sp, st);
   else if (sp.tw == 2 && sp.rg == RG) e = launch_kv8_shared<T, DH, RG, 2>(p, sp, st);
   else if (sp.tw == 2) e = launch_kv8_shared<T, DH, 1, 2>(p, sp, st);
   else e = launch_kv8_direct<T, DH>(p, sp, st);
