@@ -493,8 +493,11 @@ size_t dflow_kv8_attention_workspace(int dtype, int nseq, int max_rows, int max_
  * DFLOW_STATUS_CAPACITY.  Keys of a page whose id is outside the pool are not
  * seen (DFLOW_STATUS_BAD_PAGE).  Bytes behind a sequence's end may be anything.
  * Scores, sums and outputs are held in fp32; bf16 rows round probabilities to 11
- * bits, fp32 rows to 22.  workspace: device, 16-byte aligned, used by one call
- * at a time (calls and graphs that share it must not overlap). */
+ * bits, fp32 rows to 22.  workspace: device, 16-byte aligned, its first
+ * DFLOW_KV8_WORKSPACE_ZEROED bytes zero before its first call (every call leaves
+ * them zero), used by one call at a time (calls and graphs that share it must
+ * not overlap). */
+#define DFLOW_KV8_WORKSPACE_ZEROED 4096
 int dflow_kv8_attention(hipStream_t stream, int dtype, const dflow_kv8* cache, int nseq, const int32_t* page_table,
                         int max_pages, const int32_t* kv_len, const int32_t* row_start, int rows, int max_rows,
                         int max_len, int n_heads, const void* q, size_t ld_q, float scale, int causal, void* out,

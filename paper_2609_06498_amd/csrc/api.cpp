@@ -111,6 +111,7 @@ static constexpr int CLS_ATTN = 7;
 static constexpr int MAX_ROWS = 1024;
 
 static constexpr int PROF_MAX = 16384;
+static_assert(DFLOW_KV8_WORKSPACE_ZEROED == KV8_COUNTERS * 4, "the header states the counters' size");
 static_assert(DFLOW_SAMPLE_SCRATCH_BYTES == SAMPLE_SCRATCH_BYTES, "the header states the scratch size");
 
 extern "C" const char* dflow_last_error(void) { return g_err.c_str(); }

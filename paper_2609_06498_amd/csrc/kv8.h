@@ -54,9 +54,10 @@ struct Kv8AttnParams {
   int key_cap;               // keys read at most: min(max_len, 64 max_pages)
   int causal;
   int cus;
-  float* part;               // split partials, kv8_attn_workspace bytes
+  float* part;               // arrival counters and split partials, kv8_attn_workspace bytes
   int* status;
 };
+constexpr int KV8_COUNTERS = 1024;   // 4-byte arrival counters at the start of the workspace, zero between calls
 size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus);
 hipError_t launch_kv8_attention(bool bf16, const Kv8AttnParams& p, hipStream_t s);
 

@@ -231,16 +231,39 @@ __device__ __forceinline__ void kv8_nan_values(V&& vrun, int key16, int lim_last
   }
 }
 
+// What a workgroup does: its rows and its pages.
+struct Kv8Item {
+  int s, kvh, split, tile, G, R, nact, p0, p1;
+  Kv8Rows rows;
+};
+
+// two floats of a partial, past the XCD's cache
+__device__ __forceinline__ void kv8_put2(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 kv8_get2(const float* p) {
+  const uint64_t u = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+}
+
 // Merges the states of a row tile's PW page waves, halves at a time, through LDS
-// (TW (PW / 2) RG (DH / 4 + 2) 256 bytes; every wave is done with what it held), and
-// stores page wave 0's: the output where the rows have one split, else a partial.
+// (TW (PW / 2) RG (DH / 4 + 2) 256 bytes; every wave is done with what it held).
+// Rows with one split are stored from there; else the workgroup leaves its
+// partial in the workspace.  A single row group (PW = 4): the last of its nact
+// workgroups to arrive (a counter each, zero between launches) merges all of them
+// in split order; partials then are written and read at device scope, since these
+// workgroups may run on different XCDs, whose caches are not coherent.  (4096 keys, one
+// row: 14.3 -> 11.6 us against a launch for it.)  More rows: the combine kernel,
+// since one workgroup would read all of a tile's partials (64 rows of 32 splits: 17.4
+// against 40 us).
 template <typename T, int DH, int RG, int TW, int PW>
-__device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Split& sp, const Kv8Rows& rows, int s, int kvh,
-                                           int split, int nact, int R, int r0, int tw, int pw, float* smem, float (&M)[RG],
-                                           float (&l)[RG], f32x4_t (&o)[RG][DH / 16]) {
+__device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Split& sp, const Kv8Item& it, int r0, int tw,
+                                           int pw, float* smem, float (&M)[RG], float (&l)[RG],
+                                           f32x4_t (&o)[RG][DH / 16]) {
   constexpr int DT = DH / 16, REC = (DT * 4 + 2) * 64;   // floats of a row group's state, register by register
+  constexpr int PREC = 16 * DH + 32;                     // of a partial: outputs, then (M, l) of 16 rows
   const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
-  const int Hkv = p.c.Hkv, G = p.Hq / Hkv;
 #pragma unroll
   for (int x = 0; x < RG; ++x) {               // the row's sum over the lane groups
     float a, b;
@@ -281,29 +304,99 @@ __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Spli
     }
     __syncthreads();
   }
-  if (pw != 0) return;
+  auto store = [&](int r, int d, const float* y, float sum) {   // channels 16 d + 4 g .. of row r
+    float v[4];
 #pragma unroll
-  for (int x = 0; x < RG; ++x) {
-    const int r = r0 + x * 16 + m16;
-    if (r - m16 >= R) break;                   // uniform
-    if (nact == 1) {
-      if (r >= R) continue;
-      const int j = r / G, col = (kvh * G + r - j * G) * DH + 4 * g;
+    for (int e = 0; e < 4; ++e) v[e] = sum == 0.f ? 0.f : y[e] / sum;
+    const int j = r / it.G;
+    kv8_store4<T>(p, it.rows.start + j, (it.kvh * it.G + r - j * it.G) * DH + 16 * d + 4 * g, v);
+  };
+  if (it.nact == 1) {                          // uniform
+    if (pw != 0) return;
+#pragma unroll
+    for (int x = 0; x < RG; ++x) {
+      const int r = r0 + x * 16 + m16;
+      if (r >= it.R) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = l[x] == 0.f ? 0.f : o[x][d][e] / l[x];
-        kv8_store4<T>(p, rows.start + j, col + d * 16, y);
+        const float y[4] = {o[x][d][0], o[x][d][1], o[x][d][2], o[x][d][3]};
+        store(r, d, y, l[x]);
       }
-    } else {
-      const size_t idx = (((size_t)s * Hkv + kvh) * sp.tiles * TW * RG + r / 16) * sp.nsplit + split;
-      float* rec = p.part + idx * (16 * DH + 32);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<float4*>(rec + (d * 64 + lane) * 4) = make_float4(o[x][d][0], o[x][d][1], o[x][d][2], o[x][d][3]);
-      if (lane < 16) *reinterpret_cast<float2*>(rec + 16 * DH + 2 * lane) = make_float2(M[x], l[x]);
     }
+    return;
+  }
+  constexpr bool FUSED = TW * RG == 1;
+  const size_t item = ((size_t)it.s * p.c.Hkv + it.kvh) * sp.tiles + it.tile;
+  float* base = p.part + KV8_COUNTERS + item * TW * RG * sp.nsplit * PREC;   // [row group][split]
+  if (pw == 0) {
+#pragma unroll
+    for (int x = 0; x < RG; ++x) {
+      if (r0 + x * 16 >= it.R) break;          // uniform
+      float* rec = base + ((size_t)(tw * RG + x) * sp.nsplit + it.split) * PREC;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        float* at = rec + (d * 64 + lane) * 4;
+        if constexpr (FUSED) {
+          kv8_put2(at, o[x][d][0], o[x][d][1]);
+          kv8_put2(at + 2, o[x][d][2], o[x][d][3]);
+        } else {
+          *reinterpret_cast<float4*>(at) = make_float4(o[x][d][0], o[x][d][1], o[x][d][2], o[x][d][3]);
+        }
+      }
+      if (lane < 16) {
+        if constexpr (FUSED) kv8_put2(rec + 16 * DH + 2 * lane, M[x], l[x]);
+        else *reinterpret_cast<float2*>(rec + 16 * DH + 2 * lane) = make_float2(M[x], l[x]);
+      }
+    }
+  }
+  if constexpr (!FUSED) return;
+  unsigned* arrive = reinterpret_cast<unsigned*>(p.part) + item;   // nsplit > 1: at most KV8_COUNTERS items
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  unsigned* flag = reinterpret_cast<unsigned*>(smem);
+  if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(arrive, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (*flag != (unsigned)it.nact - 1) return;  // uniform
+  if (threadIdx.x == 0) __hip_atomic_store(arrive, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  constexpr int U = 8, DU = DT / PW;           // splits at a time, output tiles of a wave
+  const int d0 = pw * DU, r = r0 + m16;
+  const float* rec = base;
+  {
+    float m = -INFINITY, sum = 0.f, y[DU][4];
+#pragma unroll
+    for (int d = 0; d < DU; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[d][e] = 0.f;
+    for (int i = 0; i < it.nact; i += U) {     // (past the last split: it again, unused)
+      float2 ml[U], v[U][DU][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float* at = rec + (size_t)min(i + u, it.nact - 1) * PREC;
+        ml[u] = kv8_get2(at + 16 * DH + 2 * m16);
+#pragma unroll
+        for (int d = 0; d < DU; ++d) {
+          v[u][d][0] = kv8_get2(at + ((d0 + d) * 64 + lane) * 4);
+          v[u][d][1] = kv8_get2(at + ((d0 + d) * 64 + lane) * 4 + 2);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float mi = i + u < it.nact ? ml[u].x : -INFINITY;
+        const float mn = fmaxf(m, mi);
+        const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float f2 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mn);
+        const bool on = i + u < it.nact;       // (NaN of a partial stays NaN, an unused one adds nothing)
+        sum = sum * f1 + (on ? ml[u].y * f2 : 0.f);
+#pragma unroll
+        for (int d = 0; d < DU; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[d][e] = y[d][e] * f1 + (on ? (e & 1 ? v[u][d][e / 2].y : v[u][d][e / 2].x) * f2 : 0.f);
+        m = mn;
+      }
+    }
+    if (r >= it.R) return;
+#pragma unroll
+    for (int d = 0; d < DU; ++d) store(r, d0 + d, y[d], sum);
   }
 }
 
@@ -413,12 +506,7 @@ struct Kv8Wave {
   }
 };
 
-// What a workgroup does: its rows and its pages.
-struct Kv8Item {
-  int s, kvh, split, tile, G, R, nact, p0, p1;
-  Kv8Rows rows;
-};
-// false: nothing to do (uniform).  pid0: a page id loaded for page p0 + first + step lane of the table row
+// false: nothing to do (uniform).  pid: the table's id of page p0 + first + step lane
 __device__ __forceinline__ bool kv8_item(const Kv8AttnParams& p, const Kv8Split& sp, int tile_rows, int first, int step,
                                          Kv8Item& it, int& pid) {
   const int Hkv = p.c.Hkv;
@@ -444,14 +532,45 @@ __device__ __forceinline__ bool kv8_item(const Kv8AttnParams& p, const Kv8Split&
   it.p1 = min(it.p0 + sp.split_pages, (lim + PAGE - 1) / PAGE);
   return it.split < it.nact;
 }
-// invalid ids among the lane's np pages become -1 and set the status; whether there is one
-__device__ __forceinline__ bool kv8_check_ids(const Kv8AttnParams& p, int np, int& pid) {
-  const bool bad = (int)(threadIdx.x & 63) < np && (pid < 0 || pid >= p.c.num_pages);
-  if (bad) pid = -1;
-  const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
-  if (any && (threadIdx.x & 63) == 0) set_status(p.status, ST_BAD_PAGE);
-  return any;
-}
+// A wave's pages p0 + first + step i, i < np: their ids 64 at a time, a lane
+// each, taken in order; page i's validity stays known until page i + 32 is taken.
+struct Kv8Pages {
+  int pid, np;
+  uint32_t ok;
+  bool any_bad;                                // some page has an invalid id
+  __device__ __forceinline__ void load(const Kv8AttnParams& p, const Kv8Item& it, int i, int first, int step) {
+    pid = p.page_table[(size_t)it.s * p.max_pages + min(it.p0 + first + step * (i + (int)(threadIdx.x & 63)), p.max_pages - 1)];
+  }
+  __device__ __forceinline__ bool check(const Kv8AttnParams& p, int i0) {   // invalid ids become -1
+    const bool bad = i0 + (int)(threadIdx.x & 63) < np && (pid < 0 || pid >= p.c.num_pages);
+    if (bad) pid = -1;
+    return __builtin_amdgcn_ballot_w64(bad) != 0;
+  }
+  __device__ __forceinline__ Kv8Pages(const Kv8AttnParams& p, const Kv8Item& it, int pid0, int n, int first, int step)
+      : pid(pid0), np(n), ok(0), any_bad(false) {
+    if (np > 64) {                             // uniform
+      for (int i = (np - 1) & ~63; i > 0; i -= 64) {
+        load(p, it, i, first, step);
+        any_bad |= check(p, i);
+      }
+      pid = pid0;
+    }
+    any_bad |= check(p, 0);
+    if (any_bad && (threadIdx.x & 63) == 0) set_status(p.status, ST_BAD_PAGE);
+  }
+  // id of page i (0 for an invalid one: read, and not used)
+  __device__ __forceinline__ int take(const Kv8AttnParams& p, const Kv8Item& it, int i, int first, int step) {
+    if (i > 0 && (i & 63) == 0) {              // uniform
+      load(p, it, i, first, step);
+      (void)check(p, i);
+    }
+    const int v = __builtin_amdgcn_readlane(pid, i & 63);
+    const uint32_t bit = 1u << (i & 31);
+    ok = v >= 0 ? ok | bit : ok & ~bit;
+    return max(v, 0);
+  }
+  __device__ __forceinline__ bool valid(int i) const { return ok >> (i & 31) & 1; }
+};
 
 template <typename T, int DH>
 __global__ void __launch_bounds__(256, 2) kv8_direct_kernel(Kv8AttnParams p, Kv8Split sp) {
@@ -464,14 +583,14 @@ __global__ void __launch_bounds__(256, 2) kv8_direct_kernel(Kv8AttnParams p, Kv8
   int pid;
   if (!kv8_item(p, sp, RG * 16, pw, PW, it, pid)) return;
   const int Hkv = p.c.Hkv, r0 = it.tile * RG * 16, pbase = it.p0 + pw;
-  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // page pbase + PW i: id i in lane i (np <= 64)
-  const bool any_bad = kv8_check_ids(p, np, pid);
+  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // pages pbase + PW i
+  Kv8Pages pages(p, it, pid, np, pw, PW);
   u32x4_t kr[4][W::KI], vr[W::DT];
+  size_t ph = 0;                               // (page, head) block of the last page asked for
   float ksn, vsn;
   const uint32_t koff = (16 * (m16 >> 2) + (m16 & 3)) * DH + g * 16, voff = m16 * 64 + g * 16;
-  auto head = [&](int i) { return (size_t)max(__builtin_amdgcn_readlane(pid, i), 0) * Hkv + it.kvh; };   // invalid: page 0, unused
   auto issue_k = [&](int i) {
-    const size_t ph = head(i);
+    ph = (size_t)pages.take(p, it, i, pw, PW) * Hkv + it.kvh;
     const uint8_t* kb = p.c.k + ph * PAGE * DH;
     ksn = *(const gf32*)(p.c.ks + ph * 4 + g);
     vsn = *(const gf32*)(p.c.vs + ph * 4 + g);
@@ -480,32 +599,30 @@ __global__ void __launch_bounds__(256, 2) kv8_direct_kernel(Kv8AttnParams p, Kv8
 #pragma unroll
       for (int c = 0; c < W::KI; ++c) kr[kt][c] = *(const gu4*)(kb + 4 * kt * DH + c * 64 + koff);
   };
-  auto issue_v = [&](int i) {
-    const uint8_t* vb = p.c.v + head(i) * PAGE * DH;
+  auto issue_v = [&]() {
+    const uint8_t* vb = p.c.v + ph * PAGE * DH;
 #pragma unroll
     for (int d = 0; d < W::DT; ++d) vr[d] = *(const gu4*)(vb + d * 1024 + voff);
   };
   if (np > 0) {
     issue_k(0);
-    issue_v(0);
+    issue_v();
   }
   W w;
   w.load(p, it.rows, it.kvh, it.G, r0, it.R);
   const int lim_first = it.rows.limit(r0 / it.G, p.causal);
   auto step = [&]<bool EDGE>(int i, std::integral_constant<bool, EDGE>) {
-    const int kp0 = (pbase + PW * i) * PAGE;
-    w.template page<EDGE>(
-        kp0, __builtin_amdgcn_readlane(pid, i) >= 0, kr, [&](int d) { return vr[d]; }, ksn, vsn, [&]() {
-          if (i + 1 < np) issue_k(i + 1);
-        });
-    if (i + 1 < np) issue_v(i + 1);
+    w.template page<EDGE>((pbase + PW * i) * PAGE, pages.valid(i), kr, [&](int d) { return vr[d]; }, ksn, vsn, [&]() {
+      if (i + 1 < np) issue_k(i + 1);
+    });
+    if (i + 1 < np) issue_v();
   };
   // whole pages first, then those that some row sees in part (all, if an id is invalid)
-  const int full = any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
+  const int full = pages.any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
   int i = 0;
   for (; i < full; ++i) step(i, std::integral_constant<bool, false>());
   for (; i < np; ++i) step(i, std::integral_constant<bool, true>());
-  kv8_finish<T, DH, RG, 1, PW>(p, sp, it.rows, it.s, it.kvh, it.split, it.nact, it.R, r0, 0, pw, kv8_smem, w.M, w.l, w.o);
+  kv8_finish<T, DH, RG, 1, PW>(p, sp, it, r0, 0, pw, kv8_smem, w.M, w.l, w.o);
 }
 
 // 64 lanes x 4 bytes from base + voff to LDS bytes lds .. lds + 255
@@ -541,9 +658,9 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
   int pid;
   if (!kv8_item(p, sp, TW * RG * 16, pw, PW, it, pid)) return;
   const int Hkv = p.c.Hkv, r0 = (it.tile * TW + tw) * RG * 16, pbase = it.p0 + pw;
-  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // page pbase + PW i: id i in lane i (np <= 64)
+  const int np = it.p1 > pbase ? (it.p1 - pbase + PW - 1) / PW : 0;   // pages pbase + PW i
   const int steps = it.p1 > it.p0 ? (it.p1 - it.p0 + PW - 1) / PW : 0;   // of the workgroup
-  const bool any_bad = kv8_check_ids(p, np, pid);
+  Kv8Pages pages(p, it, pid, np, pw, PW);
   unsigned char* ring = reinterpret_cast<unsigned char*>(kv8_smem) + pw * NS * SLOT;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)kv8_smem + pw * NS * SLOT;
   const uint32_t koff = (16 * (m16 >> 2) + (m16 & 3)) * DH + g * 16, voff = m16 * 64 + g * 16, soff = g * 4;
@@ -556,7 +673,7 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
 #pragma unroll
     for (int k = 0; k < W::KS; ++k) asm volatile("" ::"v"(w.qf[x][k][0]));   // the rows are in before the ring's loads are counted
   auto issue = [&](int i, uint32_t slot) {     // the wave's part of page i
-    const size_t ph = (size_t)max(__builtin_amdgcn_readlane(pid, i), 0) * Hkv + it.kvh;   // invalid: page 0, unused
+    const size_t ph = (size_t)pages.take(p, it, i, pw, PW) * Hkv + it.kvh;
     const uint32_t l = lds0 + slot * SLOT;
     const uint8_t* kb = p.c.k + ph * PAGE * DH;
     const uint8_t* vb = p.c.v + ph * PAGE * DH;
@@ -596,14 +713,14 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
       read_keys(slot);
       __builtin_amdgcn_sched_barrier(0);
     }
-    w.template page<EDGE>((pbase + PW * i) * PAGE, __builtin_amdgcn_readlane(pid, i) >= 0, kk,
+    w.template page<EDGE>((pbase + PW * i) * PAGE, pages.valid(i), kk,
                           [&](int d) { return runs[(4 * W::KI + d) * 64]; }, ksc, vsc, [&]() {
                             if constexpr (AHEAD) read_keys(slot + 1 == NS ? 0 : slot + 1);   // (past the last page: unused)
                           });
   };
   auto next = [&]() { slot = slot + 1 == NS ? 0 : slot + 1; };
   // whole pages first, then those that some row sees in part (all, if an id is invalid)
-  const int full = !own || any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
+  const int full = !own || pages.any_bad ? 0 : min(np, max(0, (lim_first / PAGE - pbase + PW - 1) / PW));
   int i = 0;
   if (AHEAD && steps > 0) {
     if (np >= NS - 1) wait_barrier<(NS - 2) * LPW>();
@@ -618,7 +735,7 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
     begin(i);
     if (own && i < np && (pbase + PW * i) * PAGE < w.lim_last) step(i, std::integral_constant<bool, true>());   // uniform
   }
-  kv8_finish<T, DH, RG, TW, PW>(p, sp, it.rows, it.s, it.kvh, it.split, it.nact, it.R, r0, tw, pw, kv8_smem, w.M, w.l, w.o);
+  kv8_finish<T, DH, RG, TW, PW>(p, sp, it, r0, tw, pw, kv8_smem, w.M, w.l, w.o);
 }
 
 // Merges the splits of one 16-row group in split order: wave d the 16 channels
@@ -636,7 +753,7 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
   const int tile_end = min((rg / tile_rg + 1) * tile_rg * 16, R);
   const int nact = kv8_active(rows.limit((tile_end - 1) / G, p.causal), sp.split_pages);
   if (nact == 1) return;
-  const float* rec = p.part + (((size_t)s * Hkv + kvh) * rgs + rg) * sp.nsplit * (16 * DH + 32);
+  const float* rec = p.part + KV8_COUNTERS + (((size_t)s * Hkv + kvh) * rgs + rg) * sp.nsplit * (16 * DH + 32);
   const int r = rg * 16 + (lane & 15);
   constexpr int REC = 16 * DH + 32, U = 8;
   const float* pv = rec + (d * 64 + lane) * 4;
@@ -657,11 +774,12 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
       const float mn = fmaxf(M, mi);
       const float f1 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
       const float f2 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mn);
-      l = l * f1 + (f2 == 0.f ? 0.f : ml[u].y * f2);
-      y[0] = y[0] * f1 + (f2 == 0.f ? 0.f : v[u].x * f2);
-      y[1] = y[1] * f1 + (f2 == 0.f ? 0.f : v[u].y * f2);
-      y[2] = y[2] * f1 + (f2 == 0.f ? 0.f : v[u].z * f2);
-      y[3] = y[3] * f1 + (f2 == 0.f ? 0.f : v[u].w * f2);
+      const bool on = i + u < nact;            // (NaN of a partial stays NaN, an unused one adds nothing)
+      l = l * f1 + (on ? ml[u].y * f2 : 0.f);
+      y[0] = y[0] * f1 + (on ? v[u].x * f2 : 0.f);
+      y[1] = y[1] * f1 + (on ? v[u].y * f2 : 0.f);
+      y[2] = y[2] * f1 + (on ? v[u].z * f2 : 0.f);
+      y[3] = y[3] * f1 + (on ? v[u].w * f2 : 0.f);
       M = mn;
     }
   }
@@ -676,7 +794,8 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
 // kernel; more: as many row tiles of a workgroup's four waves as the rows fill,
 // the other waves on pages.  Pages per split: so that
 // the launch has about two workgroups per compute unit if every sequence reaches
-// key_cap, at least one page per page wave, at most 64 (a page id per lane).
+// key_cap, at least one page per page wave.  So a launch that splits has at most
+// as many row tiles as compute units: KV8_COUNTERS bounds them.
 inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int cus) {
   const long long R = (long long)max_rows * (Hq / Hkv);
   Kv8Split sp;
@@ -685,19 +804,19 @@ inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq
   sp.tw = R <= per ? 1 : (R <= 2 * per ? 2 : 4);
   sp.pw = 4 / sp.tw;
   sp.tiles = (int)((R + per * sp.tw - 1) / (per * sp.tw));
+  if (cus > KV8_COUNTERS) cus = KV8_COUNTERS;
   const long long items = (long long)nseq * Hkv * sp.tiles;
   const int pages = key_cap > 0 ? (key_cap + PAGE - 1) / PAGE : 1;
   const long long want = items < 2 * cus ? 2 * cus / items : 1;
   long long pp = (pages + want - 1) / want;
   if (pp < sp.pw) pp = sp.pw;
-  if (pp > 64 * sp.pw) pp = 64 * sp.pw;
   sp.split_pages = (int)pp;
   sp.nsplit = (int)((pages + pp - 1) / pp);
   return sp;
 }
 
 inline size_t kv8_part_floats(const Kv8Split& sp, int nseq, int Hkv, int Dh) {
-  return sp.nsplit == 1 ? 0 : (size_t)nseq * Hkv * sp.tiles * sp.tw * sp.rg * sp.nsplit * (16 * Dh + 32);
+  return sp.nsplit == 1 ? 0 : KV8_COUNTERS + (size_t)nseq * Hkv * sp.tiles * sp.tw * sp.rg * sp.nsplit * (16 * Dh + 32);
 }
 
 template <auto KERNEL>
@@ -708,6 +827,12 @@ static hipError_t launch_kv8_kernel(const Kv8AttnParams& p, const Kv8Split& sp, 
   const long long wgs = (long long)p.nseq * p.c.Hkv * sp.tiles * sp.nsplit;
   if (wgs > 0x7FFFFFFFll) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(KERNEL, dim3((unsigned)wgs), dim3(threads), lds, st, p, sp);
+  return hipGetLastError();
+}
+template <typename T, int DH>
+static hipError_t launch_kv8_combine(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
+  hipLaunchKernelGGL((kv8_combine_kernel<T, DH>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.tw * sp.rg), dim3(DH * 4), 0, st,
+                     p, sp);
   return hipGetLastError();
 }
 
@@ -724,21 +849,18 @@ static hipError_t launch_kv8_shared(const Kv8AttnParams& p, const Kv8Split& sp, 
   constexpr int PW = KV8_SHARED_WAVES / TW;
   constexpr size_t ring = (size_t)PW * kv8_slots(PW) * kv8_slot_bytes<DH>();
   constexpr size_t merge = kv8_merge_bytes(DH, RG, TW, PW);
-  return launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, KV8_SHARED_WAVES * 64, ring > merge ? ring : merge, st);
+  const hipError_t e =
+      launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, KV8_SHARED_WAVES * 64, ring > merge ? ring : merge, st);
+  return e != hipSuccess || sp.nsplit == 1 ? e : launch_kv8_combine<T, DH>(p, sp, st);
 }
 
 template <typename T, int DH>
 static hipError_t launch_kv8_dh(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
   constexpr int RG = sizeof(T) == 2 ? 2 : 1;
-  hipError_t e;
-  if (sp.tw == 4) e = launch_kv8_shared<T, DH, RG, 4>(p, sp, st);
-  else if (sp.tw == 2 && sp.rg == RG) e = launch_kv8_shared<T, DH, RG, 2>(p, sp, st);
-  else if (sp.tw == 2) e = launch_kv8_shared<T, DH, 1, 2>(p, sp, st);
-  else e = launch_kv8_direct<T, DH>(p, sp, st);
-  if (e != hipSuccess || sp.nsplit == 1) return e;
-  hipLaunchKernelGGL((kv8_combine_kernel<T, DH>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.tw * sp.rg), dim3(DH * 4), 0, st,
-                     p, sp);
-  return hipGetLastError();
+  if (sp.tw == 4) return launch_kv8_shared<T, DH, RG, 4>(p, sp, st);
+  if (sp.tw == 2 && sp.rg == RG) return launch_kv8_shared<T, DH, RG, 2>(p, sp, st);
+  if (sp.tw == 2) return launch_kv8_shared<T, DH, 1, 2>(p, sp, st);
+  return launch_kv8_direct<T, DH>(p, sp, st);
 }
 
 size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus) {

@@ -138,6 +138,14 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
       uint8_t* dst = p.c.v + (ph * DH + c0) * PAGE + part * KV8_GROUP;
       float x[CL][KV8_GROUP];
       uint4 was[CL];
+      // every load in flight at once: a token that is not appended reads the run's first row, unused
+      T raw[KV8_GROUP][CL];
+#pragma unroll
+      for (int t = 0; t < KV8_GROUP; ++t) {
+        const int sr = __builtin_amdgcn_readlane(src, t);
+        const T* v = reinterpret_cast<const T*>(p.v) + (size_t)(sr >= 0 ? sr : r0 - 1 + ld) * p.ld_v + (size_t)h * DH + c0;
+        __builtin_memcpy(raw[t], __builtin_assume_aligned(v, CL * sizeof(T)), CL * sizeof(T));
+      }
 #pragma unroll
       for (int c = 0; c < CL; ++c) {
         was[c] = make_uint4(0, 0, 0, 0);
@@ -145,20 +153,12 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
       }
 #pragma unroll
       for (int t = 0; t < KV8_GROUP; ++t) {
-        const int sr = __builtin_amdgcn_readlane(src, t);
-        if (sr >= 0) {
-          const T* v = reinterpret_cast<const T*>(p.v) + (size_t)sr * p.ld_v + (size_t)h * DH + c0;
 #pragma unroll
-          for (int c = 0; c < CL; ++c) x[c][t] = TT<T>::ld(v, c);
-        } else {
-          const uint32_t sel = t / 4;
-#pragma unroll
-          for (int c = 0; c < CL; ++c) {
-            const uint32_t u = sel == 0 ? was[c].x : sel == 1 ? was[c].y : sel == 2 ? was[c].z : was[c].w;
-            float y[4];
-            kv8_unpack4(u, old, y);
-            x[c][t] = t < t0 ? y[t & 3] : 0.f;
-          }
+        for (int c = 0; c < CL; ++c) {
+          const uint32_t u = t / 4 == 0 ? was[c].x : t / 4 == 1 ? was[c].y : t / 4 == 2 ? was[c].z : was[c].w;
+          float y[4];
+          kv8_unpack4(u, old, y);
+          x[c][t] = fresh >> t & 1 ? TT<T>::ld(raw[t], c) : t < t0 ? y[t & 3] : 0.f;
         }
       }
       float amax = 0.f;

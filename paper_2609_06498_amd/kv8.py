@@ -20,6 +20,7 @@ from typing import Optional
 from .runtime import DFLOW_BF16, DFLOW_F32, KV8, PAGE, DFlowError, Pool, load_library
 
 GROUP = 16                     # tokens per scale
+WORKSPACE_ZEROED = 4096        # DFLOW_KV8_WORKSPACE_ZEROED
 
 
 def _same_device(dev, **tensors):
@@ -195,6 +196,7 @@ class KV8Cache(_DeviceCalls):
                 self._kept.append(self._ws)
             self._ws_bytes = max(need, 2 * self._ws_bytes)
             self._ws = self.torch.empty(self._ws_bytes, dtype=self.torch.uint8, device=self.device)
+            self._ws[:WORKSPACE_ZEROED].zero_()
 
     def attention(self, q, page_table, kv_len, row_start, max_rows: int, max_len: int, causal: bool = True,
                   scale: Optional[float] = None, out=None):

@@ -166,6 +166,19 @@ def test_attention_nan_that_some_rows_see(dtype):
         assert (np.abs(out - want)[~nan] <= bound[~nan]).all()
 
 
+@pytest.mark.parametrize("rows", [1, 16])
+def test_attention_nan_keys_of_a_whole_head(rows):
+    """Every key of a head NaN, over several splits: its rows are NaN, the other head's are not."""
+    rng = np.random.default_rng(16)
+    n = 500
+    c = random_cache(8, 2, 64, rng)
+    c.code["k"][:, 1] = 0x7F
+    t = np.arange(8, dtype=np.int32)[None]
+    q = rounded(rng.normal(0, 1, (rows, 8, 64)), "bf16")
+    out = upload(c).attention(dev(q, torch.bfloat16), i32(t), i32([n]), i32([0, rows]), rows, n)
+    assert out[:, 4:].isnan().all() and not out[:, :4].isnan().any()
+
+
 def test_attention_large_and_small_magnitudes():
     """Scales from 2^-60 to 2^60 in one sequence, scores far apart: the softmax picks what 64 bits pick."""
     rng = np.random.default_rng(7)
