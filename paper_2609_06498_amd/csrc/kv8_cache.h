@@ -1,5 +1,7 @@
 // Writes of the paged 8-bit cache and its page table (included by elementwise.hip).
 #pragma once
+#include <limits.h>
+
 #include "common.h"
 #include "kernels.h"
 #include "kv8.h"
@@ -217,123 +219,141 @@ hipError_t launch_kv8_append(bool isbf, const Kv8AppendParams& p, hipStream_t st
 constexpr int PAGES_T = 1024;
 constexpr int PAGES_INLINE_ROWS = 4096;
 
-// exclusive sum over the workgroup's threads; *total: the sum
-__device__ inline long long block_scan(long long v, long long* sh /* [17] */, long long* total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  long long x = v;
+// exclusive sums of three values over the workgroup's threads, and their totals
+struct Sum3 { long long v[3]; };
+__device__ inline Sum3 block_scan(const Sum3& x, Sum3* sh /* [16] */, Sum3* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  Sum3 s = x;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) sh[w] = x;
-  __syncthreads();
-  long long base = 0, all = 0;
+  for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
-  for (int i = 0; i < PAGES_T / 64; ++i) {
-    if (i < w) base += sh[i];
-    all += sh[i];
-  }
+    for (int i = 0; i < 3; ++i) {
+      const long long y = __shfl_up(s.v[i], o, 64);
+      if (lane >= o) s.v[i] += y;
+    }
+  if (lane == 63) sh[w] = s;
+  __syncthreads();
+  Sum3 base{{0, 0, 0}}, all{{0, 0, 0}};
+  for (int k = 0; k < nw; ++k)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (k < w) base.v[i] += sh[k].v[i];
+      all.v[i] += sh[k].v[i];
+    }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) s.v[i] += base.v[i] - x.v[i];
   *total = all;
-  return base + x - v;
+  return s;
 }
 
-// slot of row r of the call: sequence by binary search over the row starts
-__device__ inline int map_slot(const PageResizeParams& p, const int* starts, int r) {
+// slot of row r of the call: sequence by binary search over the row starts.
+// base(s): tokens the sequence had, -1 where it was refused.
+template <typename F>
+__device__ inline int map_slot(const PageResizeParams& p, const int* starts, F&& base, int r) {
   int lo = 0, hi = p.nseq;                     // starts[lo] <= r < starts[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (starts[mid] <= r) lo = mid;
     else hi = mid;
   }
-  const long long len = p.seq_len[lo], nw = p.new_len[lo];
-  if (len < 0 || (len + nw + PAGE - 1) / PAGE > p.n_held[lo]) return -1;   // refused
-  const int pos = (int)len + r - starts[lo];
+  const int len = base(lo);
+  if (len < 0) return -1;
+  const int pos = len + r - starts[lo];
   const int page = p.page_table[(size_t)lo * p.max_pages + pos / PAGE];
   return page < 0 || page >= p.num_pages ? -1 : page * PAGE + pos % PAGE;
 }
 
 __global__ void __launch_bounds__(PAGES_T) page_resize_kernel(PageResizeParams p, int inline_slots) {
-  __shared__ long long sh[17];
-  __shared__ int s_held[PAGES_MAX_SEQ], s_cnt[PAGES_MAX_SEQ], s_off[PAGES_MAX_SEQ], s_start[PAGES_MAX_SEQ + 1];
-  const int s = threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  __shared__ Sum3 sh[PAGES_T / 64];
+  __shared__ int s_held[PAGES_MAX_SEQ], s_drop[PAGES_MAX_SEQ], s_doff[PAGES_MAX_SEQ], s_take[PAGES_MAX_SEQ],
+      s_toff[PAGES_MAX_SEQ], s_len[PAGES_MAX_SEQ], s_start[PAGES_MAX_SEQ + 1], s_taken;
+  const int s = threadIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
   const bool have = s < p.nseq;
-  const long long len = have ? p.seq_len[s] : 0, nw = have && p.new_len ? p.new_len[s] : 0;
-  const int top0 = *p.n_free;
+  const int sc = min(s, p.nseq - 1);
+  const long long len = p.seq_len[sc], more = p.new_len ? p.new_len[sc] : 0;
+  const int held0 = p.n_held[sc], top0 = *p.n_free;
+  if (s == 0) s_taken = 0;
   int bits = top0 < 0 || top0 > p.num_pages ? ST_CAPACITY : 0;
   const int top = min(max(top0, 0), p.num_pages);
-  const int held0 = have ? p.n_held[s] : 0;
-  int held = min(max(held0, 0), p.max_pages);
-  const long long target = (len + nw + PAGE - 1) / PAGE;
-  const bool valid = have && len >= 0 && nw >= 0 && target <= p.max_pages;
-  if ((have && !valid) || held != held0) bits |= ST_CAPACITY;
-  // give back
+  const int held = min(max(held0, 0), p.max_pages);
+  const long long target = (len + more + PAGE - 1) / PAGE;
+  const bool valid = have && len >= 0 && more >= 0 && target <= p.max_pages;
+  if (have && (!valid || held != held0)) bits |= ST_CAPACITY;
   const int drop = valid && held > target ? held - (int)target : 0;
-  long long dropped;
-  int off = (int)block_scan(drop, sh, &dropped);
-  if (have) { s_held[s] = held - drop; s_cnt[s] = drop; s_off[s] = off; }
+  const int want = valid && target > held ? (int)target - held : 0;
+  Sum3 tot;
+  const Sum3 at = block_scan(Sum3{{drop, want, have && more > 0 ? more : 0}}, sh, &tot);
+  const long long dropped = tot.v[0], avail = min((long long)top + dropped, (long long)p.num_pages);
+  const int take = want > 0 && at.v[1] + want <= avail ? want : 0;   // (sequences that take are the first that want)
+  if (want > take) bits |= ST_CAPACITY;
+  const int cap = p.slot ? p.slot_cap : INT_MAX;
+  const bool fits = valid && want == take;
+  if (have) {
+    s_held[s] = held - drop;
+    s_drop[s] = drop;
+    s_doff[s] = (int)at.v[0];
+    s_take[s] = take;
+    s_toff[s] = (int)at.v[1];
+    s_len[s] = fits ? (int)len : -1;
+    s_start[s] = (int)min(at.v[2], (long long)cap);
+    if (take > 0) atomicMax(&s_taken, (int)at.v[1] + take);
+    if (held - drop + take != held0) p.n_held[s] = held - drop + take;
+  }
+  if (s == 0) s_start[p.nseq] = (int)min(tot.v[2], (long long)cap);
+  if (p.slot && tot.v[2] > cap) bits |= ST_CAPACITY;
   __syncthreads();
-  if (dropped > 0) {                           // uniform
-    for (int q = w; q < p.nseq; q += PAGES_T / 64)
-      for (int i = lane; i < s_cnt[q]; i += 64) {
+  if (dropped > 0) {                           // uniform: give back
+    for (int q = w; q < p.nseq; q += nw)
+      for (int i = lane; i < s_drop[q]; i += 64) {
         int* e = p.page_table + (size_t)q * p.max_pages + s_held[q] + i;
-        const long long at = top + dropped - 1 - (s_off[q] + i);
-        if (at < p.num_pages) p.free_pages[at] = *e;
+        const long long to = top + dropped - 1 - (s_doff[q] + i);
+        if (to < p.num_pages) p.free_pages[to] = *e;
         else bits |= ST_CAPACITY;              // more pages than the pool has: the caller's state is wrong
         *e = -1;
       }
     __threadfence_block();
+    __syncthreads();
   }
-  held -= drop;
-  const long long avail = min((long long)top + dropped, (long long)p.num_pages);
-  // take
-  const int want = valid && target > held ? (int)target - held : 0;
-  long long wanted;
-  const long long at = block_scan(want, sh, &wanted);     // (barriers: the pushes above are done)
-  const int take = want > 0 && at + want <= avail ? want : 0;
-  if (want > take) bits |= ST_CAPACITY;
-  long long taken;
-  block_scan(take, sh, &taken);
-  if (have) { s_held[s] = held; s_cnt[s] = take; s_off[s] = (int)at; }
-  __syncthreads();
-  if (taken > 0) {
-    for (int q = w; q < p.nseq; q += PAGES_T / 64)
-      for (int i = lane; i < s_cnt[q]; i += 64)
-        p.page_table[(size_t)q * p.max_pages + s_held[q] + i] = p.free_pages[avail - 1 - (s_off[q] + i)];
+  const int taken = s_taken;
+  if (taken > 0) {                             // uniform: take
+    for (int q = w; q < p.nseq; q += nw)
+      for (int i = lane; i < s_take[q]; i += 64)
+        p.page_table[(size_t)q * p.max_pages + s_held[q] + i] = p.free_pages[avail - 1 - (s_toff[q] + i)];
   }
-  held += take;
-  if (have && held != held0) p.n_held[s] = held;
-  if (threadIdx.x == 0) *p.n_free = (int)(avail - taken);
+  if (s == 0) *p.n_free = (int)(avail - taken);
   if (p.slot) {
-    long long rows;
-    const long long r = block_scan(nw > 0 ? nw : 0, sh, &rows);
-    if (rows > p.slot_cap) bits |= ST_CAPACITY;
-    if (have) { s_start[s] = (int)min(r, (long long)p.slot_cap); p.row_start[s] = s_start[s]; }
-    if (threadIdx.x == 0) {
-      s_start[p.nseq] = (int)min(rows, (long long)p.slot_cap);
-      p.row_start[p.nseq] = s_start[p.nseq];
-    }
+    for (int i = s; i <= p.nseq; i += blockDim.x) p.row_start[i] = s_start[i];
     if (inline_slots) {
-      __threadfence_block();
-      __syncthreads();
-      for (int i = threadIdx.x; i < s_start[p.nseq]; i += PAGES_T) p.slot[i] = map_slot(p, s_start, i);
+      if (taken > 0) {
+        __threadfence_block();
+        __syncthreads();
+      }
+      for (int i = s; i < s_start[p.nseq]; i += blockDim.x)
+        p.slot[i] = map_slot(p, s_start, [&](int q) { return s_len[q]; }, i);
     }
   }
   if (bits) set_status(p.status, bits);
 }
 
+// Slots of many rows, after page_resize_kernel: a sequence whose row is too short was refused.
 __global__ void __launch_bounds__(256) slot_map_kernel(PageResizeParams p) {
   __shared__ int starts[PAGES_MAX_SEQ + 1];
   for (int i = threadIdx.x; i <= p.nseq; i += 256) starts[i] = p.row_start[i];
   __syncthreads();
   const int r = blockIdx.x * 256 + threadIdx.x;
-  if (r < starts[p.nseq]) p.slot[r] = map_slot(p, starts, r);
+  if (r >= starts[p.nseq]) return;
+  p.slot[r] = map_slot(p, starts, [&](int q) {
+    const long long len = p.seq_len[q], more = p.new_len[q];
+    return len < 0 || (len + more + PAGE - 1) / PAGE > p.n_held[q] ? -1 : (int)len;
+  }, r);
 }
 
 hipError_t launch_page_resize(const PageResizeParams& p, hipStream_t st) {
+  // a thread per sequence; more only where there are many slots to map
   const int inl = p.slot_cap <= PAGES_INLINE_ROWS;
-  hipLaunchKernelGGL(page_resize_kernel, dim3(1), dim3(PAGES_T), 0, st, p, inl);
+  int threads = (p.nseq + 255) / 256 * 256;
+  if (p.slot && inl && p.slot_cap > 1024) threads = PAGES_T;
+  hipLaunchKernelGGL(page_resize_kernel, dim3(1), dim3(threads), 0, st, p, inl);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.slot || inl) return e;
   hipLaunchKernelGGL(slot_map_kernel, dim3((p.slot_cap + 255) / 256), dim3(256), 0, st, p);

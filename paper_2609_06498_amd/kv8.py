@@ -12,7 +12,6 @@ object's status word, which status() reads.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 from typing import Optional
@@ -23,17 +22,14 @@ GROUP = 16                     # tokens per scale
 WORKSPACE_ZEROED = 4096        # DFLOW_KV8_WORKSPACE_ZEROED
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise DFlowError(f"{name} is on {t.device}, not on {dev}")
-
-
-def _check_i32(torch, name, t, shape):
-    if t.dtype is not torch.int32 or t.dim() != len(shape) or not t.is_contiguous():
-        raise DFlowError(f"{name} must be a contiguous int32 tensor of {len(shape)} dimension(s)")
-    for have, want in zip(t.shape, shape):
-        if want is not None and have < want:
+def _refuse(index, need):
+    """Raises for the first of need = [(name, tensor, dtype, least shape or None)] that does not fit."""
+    for name, t, dt, shape in need:
+        if t.get_device() != index:
+            raise DFlowError(f"{name} is on {t.device}, not on cuda:{index}")
+        if dt is not None and (t.dtype is not dt or not t.is_contiguous()):
+            raise DFlowError(f"{name} must be contiguous {dt}, got {t.dtype} with strides {t.stride()}")
+        if shape is not None and (t.dim() != len(shape) or any(h < w for h, w in zip(t.shape, shape))):
             raise DFlowError(f"{name} has shape {tuple(t.shape)}, at least {shape} needed")
 
 
@@ -44,25 +40,26 @@ class _DeviceCalls:
         import torch
         if t.device.type != "cuda":
             raise DFlowError("the 8-bit cache needs a HIP device; there is no CPU path")
-        self.torch, self.device, self.lib = torch, t.device, load_library()
+        self.torch, self.device, self.index, self.lib = torch, t.device, t.get_device(), load_library()
         self.status_word = torch.zeros(1, dtype=torch.int32, device=t.device)
         self._status = self.status_word.data_ptr()
+        # (a call takes a few microseconds on the device: its host side avoids what is slow in Python)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._current = torch._C._cuda_getDevice
 
-    def _on(self):
-        """The device of the tensors made current (usually it is)."""
-        cuda = self.torch.cuda
-        return contextlib.nullcontext() if cuda.current_device() == self.device.index else cuda.device(self.device)
-
-    def _stream(self):
-        return self.torch.cuda.current_stream(self.device).cuda_stream
-
-    def _check(self, rc: int, what: str):
+    def _call(self, fn, *args):
+        """fn(stream, *args) on the current stream of the tensors' device, made current if it is not."""
+        if self._current() == self.index:
+            rc = fn(self._raw_stream(self.index), *args)
+        else:
+            with self.torch.cuda.device(self.index):
+                rc = fn(self._raw_stream(self.index), *args)
         if rc != 0:
-            raise DFlowError(f"{what} failed ({rc}): {self.lib.dflow_last_error().decode()}")
+            raise DFlowError(f"{fn.__name__} failed ({rc}): {self.lib.dflow_last_error().decode()}")
 
     def status(self, clear: bool = True) -> int:
         """DFLOW_STATUS_* bits set by the calls so far (waits for the current stream)."""
-        with self._on():
+        with self.torch.cuda.device(self.index):
             v = int(self.status_word.item())
             if clear and v:
                 self.status_word.zero_()
@@ -77,12 +74,9 @@ class PagePool(_DeviceCalls):
 
     def __init__(self, page_table, n_held, free_pages, n_free):
         self._open(page_table)
-        torch = self.torch
-        _same_device(self.device, n_held=n_held, free_pages=free_pages, n_free=n_free)
-        _check_i32(torch, "page_table", page_table, (1, 1))
-        _check_i32(torch, "n_held", n_held, (page_table.shape[0],))
-        _check_i32(torch, "free_pages", free_pages, (1,))
-        _check_i32(torch, "n_free", n_free, (1,))
+        i32 = self._i32 = self.torch.int32
+        _refuse(self.index, [("page_table", page_table, i32, (1, 1)), ("free_pages", free_pages, i32, (1,)),
+                             ("n_held", n_held, i32, (page_table.shape[0],)), ("n_free", n_free, i32, (1,))])
         self.page_table, self.n_held, self.free_pages, self.n_free = page_table, n_held, free_pages, n_free
         self.num_pages = free_pages.shape[0]
         self._pool = Pool(page_table.data_ptr(), page_table.shape[1], n_held.data_ptr(), free_pages.data_ptr(),
@@ -101,23 +95,22 @@ class PagePool(_DeviceCalls):
         """dflow_page_resize over the first len(seq_len) rows; with `slot` (int32
         [capacity]) also the slot map of the new tokens and their row_start
         [nseq + 1]."""
-        torch, n = self.torch, seq_len.shape[0]
-        _same_device(self.device, seq_len=seq_len, new_len=new_len, slot=slot, row_start=row_start)
-        _check_i32(torch, "seq_len", seq_len, (1,))
+        n, i, i32 = len(seq_len), self.index, self._i32
         if n > self.page_table.shape[0]:
             raise DFlowError(f"{n} sequences, {self.page_table.shape[0]} page-table rows")
-        if new_len is not None:
-            _check_i32(torch, "new_len", new_len, (n,))
-        if slot is not None:
-            if new_len is None or row_start is None:
-                raise DFlowError("a slot map needs new_len and row_start")
-            _check_i32(torch, "slot", slot, (None,))
-            _check_i32(torch, "row_start", row_start, (n + 1,))
-        p = lambda t: None if t is None else t.data_ptr()
-        with self._on():
-            self._check(self.lib.dflow_page_resize(
-                self._stream(), self._ref, n, seq_len.data_ptr(), p(new_len), p(slot),
-                0 if slot is None else slot.shape[0], p(row_start), self._status), "dflow_page_resize")
+        given = seq_len if new_len is None else (seq_len, new_len) if slot is None else (seq_len, new_len, slot, row_start)
+        if slot is not None and (new_len is None or row_start is None):
+            raise DFlowError("a slot map needs new_len and row_start")
+        cap = 0 if slot is None else slot.numel()
+        for t in (given if type(given) is tuple else (given,)):
+            if t.dtype is not i32 or t.get_device() != i or t.dim() != 1 or not t.is_contiguous():
+                _refuse(i, [("seq_len", seq_len, i32, (1,))] + [(m, x, i32, (k,)) for m, x, k in (
+                    ("new_len", new_len, n), ("slot", slot, 0), ("row_start", row_start, n + 1)) if x is not None])
+        if new_len is not None and len(new_len) < n or slot is not None and len(row_start) < n + 1:
+            raise DFlowError(f"new_len needs {n} and row_start {n + 1} entries")
+        self._call(self.lib.dflow_page_resize, self._ref, n, seq_len.data_ptr(),
+                   None if new_len is None else new_len.data_ptr(), None if slot is None else slot.data_ptr(), cap,
+                   None if slot is None else row_start.data_ptr(), self._status)
 
 
 class KV8Cache(_DeviceCalls):
@@ -128,7 +121,7 @@ class KV8Cache(_DeviceCalls):
     def __init__(self, k, v, k_scale, v_scale):
         self._open(k)
         torch = self.torch
-        _same_device(self.device, v=v, k_scale=k_scale, v_scale=v_scale)
+        _refuse(self.index, [("v", v, None, None), ("k_scale", k_scale, None, None), ("v_scale", v_scale, None, None)])
         if k.dim() != 4 or k.shape[2] != PAGE:
             raise DFlowError(f"k has shape {tuple(k.shape)}, [num_pages, n_kv_heads, {PAGE}, head_dim] needed")
         n, h, _, d = k.shape
@@ -143,7 +136,8 @@ class KV8Cache(_DeviceCalls):
         self._ref = ctypes.byref(self._kv)
         self._scale = 1.0 / math.sqrt(d)
         self._codes = {torch.bfloat16: DFLOW_BF16, torch.float32: DFLOW_F32}
-        self._ws, self._ws_bytes, self._kept = None, 0, []
+        self._i32 = torch.int32
+        self._ws, self._ws_ptr, self._ws_bytes, self._kept = None, None, 0, []
         self._need = {}
 
     @classmethod
@@ -155,48 +149,47 @@ class KV8Cache(_DeviceCalls):
         return cls(u8(num_pages, n_kv_heads, PAGE, head_dim), u8(num_pages, n_kv_heads, head_dim, PAGE), one(), one())
 
     def _rows(self, name, t, heads):
-        """(dtype code, row stride in elements) of a [rows, heads, head_dim] tensor whose rows are dense."""
+        """(rows, heads, dtype code, row stride in elements) of a [rows, heads, head_dim] tensor whose rows are dense."""
         code = self._codes.get(t.dtype)
-        if code is None:
-            raise DFlowError(f"{name} must be bfloat16 or float32, got {t.dtype}")
         n, h, d = t.shape if t.dim() == 3 else (0, 0, 0)
-        if d != self.head_dim or (heads is not None and h != heads) or h < 1:
-            raise DFlowError(f"{name} has shape {tuple(t.shape)}, [rows, {heads or 'heads'}, {self.head_dim}] needed")
+        if code is None or d != self.head_dim or h < 1 or (heads is not None and h != heads):
+            raise DFlowError(f"{name} must be bfloat16 or float32 [rows, {heads or 'heads'}, {self.head_dim}], got "
+                             f"{t.dtype} {tuple(t.shape)}")
+        if t.get_device() != self.index:
+            _refuse(self.index, [(name, t, None, None)])
+        if t.is_contiguous():
+            return n, h, code, h * d
         s = t.stride()
         if s[2] != 1 or (h > 1 and s[1] != d):
             raise DFlowError(f"{name}: the heads of a row must be contiguous (strides {s})")
-        return code, (s[0] if n > 1 else h * d)
+        return n, h, code, (s[0] if n > 1 else h * d)
 
     def append(self, k, v, slot):
         """dflow_kv8_append: rows k, v [rows, n_kv_heads, head_dim] (bf16 or fp32) to their slots (int32 [rows], -1: none)."""
-        dev, n = self.device, k.shape[0]
-        if k.device != dev or v.device != dev or slot.device != dev:
-            _same_device(dev, k=k, v=v, slot=slot)
-        code, ld_k = self._rows("k", k, self.n_kv_heads)
-        code_v, ld_v = self._rows("v", v, self.n_kv_heads)
-        if code_v != code or v.shape[0] != n:
+        n, _, code, ld_k = self._rows("k", k, self.n_kv_heads)
+        n_v, _, code_v, ld_v = self._rows("v", v, self.n_kv_heads)
+        if code_v != code or n_v != n:
             raise DFlowError(f"k {k.dtype} {tuple(k.shape)} and v {v.dtype} {tuple(v.shape)} differ")
-        _check_i32(self.torch, "slot", slot, (n,))
-        with self._on():
-            self._check(self.lib.dflow_kv8_append(self._stream(), code, self._ref, n, k.data_ptr(), ld_k, v.data_ptr(),
-                                                  ld_v, slot.data_ptr(), self._status), "dflow_kv8_append")
+        if slot.dtype is not self._i32 or slot.get_device() != self.index or slot.numel() < n or not slot.is_contiguous():
+            _refuse(self.index, [("slot", slot, self._i32, (n,))])
+        self._call(self.lib.dflow_kv8_append, code, self._ref, n, k.data_ptr(), ld_k, v.data_ptr(), ld_v, slot.data_ptr(),
+                   self._status)
 
     def _workspace(self, key):
         """Workspace for calls of these sizes.  A buffer that is outgrown is kept: graphs captured with it hold its address."""
-        need = self._need.get(key)
-        if need is None:
-            need = self.lib.dflow_kv8_attention_workspace(*key, self.n_kv_heads, self.head_dim)
-            if need == ctypes.c_size_t(-1).value:
-                self._check(-1, "dflow_kv8_attention_workspace")
-            if len(self._need) >= 4096:
-                self._need.clear()
-            self._need[key] = need
+        need = self.lib.dflow_kv8_attention_workspace(*key, self.n_kv_heads, self.head_dim)
+        if need == ctypes.c_size_t(-1).value:
+            raise DFlowError(f"dflow_kv8_attention_workspace: {self.lib.dflow_last_error().decode()}")
+        if len(self._need) >= 4096:
+            self._need.clear()
+        self._need[key] = need
         if need > self._ws_bytes:
             if self._ws is not None:
                 self._kept.append(self._ws)
             self._ws_bytes = max(need, 2 * self._ws_bytes)
             self._ws = self.torch.empty(self._ws_bytes, dtype=self.torch.uint8, device=self.device)
             self._ws[:WORKSPACE_ZEROED].zero_()
+            self._ws_ptr = self._ws.data_ptr()
 
     def attention(self, q, page_table, kv_len, row_start, max_rows: int, max_len: int, causal: bool = True,
                   scale: Optional[float] = None, out=None):
@@ -204,24 +197,25 @@ class KV8Cache(_DeviceCalls):
         len(kv_len) sequences, rows row_start[s] .. row_start[s + 1] - 1 each, over
         kv_len[s] cached tokens.  max_rows and max_len bound both.  scale
         defaults to head_dim^-1/2.  Returns out."""
-        torch, dev, n = self.torch, self.device, kv_len.shape[0]
+        rows, heads, code, ld_q = self._rows("q", q, None)
         if out is None:
-            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        _same_device(dev, q=q, page_table=page_table, kv_len=kv_len, row_start=row_start, out=out)
-        code, ld_q = self._rows("q", q, None)
-        code_o, ld_o = self._rows("out", out, q.shape[1])
-        if code_o != code or out.shape != q.shape:
+            out = self.torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        rows_o, _, code_o, ld_o = self._rows("out", out, heads)
+        if code_o != code or rows_o != rows:
             raise DFlowError(f"q {q.dtype} {tuple(q.shape)} and out {out.dtype} {tuple(out.shape)} differ")
-        _check_i32(torch, "page_table", page_table, (n, 1))
-        _check_i32(torch, "kv_len", kv_len, (1,))
-        _check_i32(torch, "row_start", row_start, (n + 1,))
-        max_pages = page_table.shape[1]
-        with self._on():
-            self._workspace((code, n, max_rows, min(max_len, max_pages * PAGE), q.shape[1]))
-            self._check(self.lib.dflow_kv8_attention(
-                self._stream(), code, self._ref, n, page_table.data_ptr(), max_pages, kv_len.data_ptr(),
-                row_start.data_ptr(), q.shape[0], max_rows, max_len, q.shape[1], q.data_ptr(), ld_q,
-                self._scale if scale is None else scale, bool(causal), out.data_ptr(), ld_o,
-                None if self._ws is None else self._ws.data_ptr(), self._ws_bytes, self._status),
-                "dflow_kv8_attention")
+        i, i32, n = self.index, self._i32, len(kv_len)
+        width = page_table.shape[-1]
+        if not (page_table.dtype is i32 and kv_len.dtype is i32 and row_start.dtype is i32
+                and page_table.is_contiguous() and kv_len.is_contiguous() and row_start.is_contiguous()
+                and page_table.get_device() == i and kv_len.get_device() == i and row_start.get_device() == i
+                and page_table.dim() == 2 and len(page_table) >= n and len(row_start) > n):
+            _refuse(i, [("page_table", page_table, i32, (n, 1)), ("kv_len", kv_len, i32, (1,)),
+                        ("row_start", row_start, i32, (n + 1,))])
+        key = (code, n, max_rows, min(max_len, width * PAGE), heads)
+        if self._need.get(key, self._ws_bytes + 1) > self._ws_bytes:
+            self._workspace(key)
+        self._call(self.lib.dflow_kv8_attention, code, self._ref, n, page_table.data_ptr(), width, kv_len.data_ptr(),
+                   row_start.data_ptr(), rows, max_rows, max_len, heads, q.data_ptr(), ld_q,
+                   self._scale if scale is None else scale, causal, out.data_ptr(), ld_o, self._ws_ptr, self._ws_bytes,
+                   self._status)
         return out
