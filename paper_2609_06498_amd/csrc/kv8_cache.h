@@ -34,21 +34,29 @@ __device__ inline int kv8_exponent(float amax) {
   return min(max(e, KV8_MIN_EXP), KV8_MAX_EXP);
 }
 __device__ inline float kv8_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-__device__ inline float kv8_finite_abs(float x) {
-  const float a = fabsf(x);
-  return a < INFINITY ? a : 0.f;               // infinities and NaN do not set a scale
-}
-// four values / 2^e as e4m3 codes: nearest even, at most 448 in magnitude, NaN stays NaN
-__device__ inline uint32_t kv8_pack4(const float* x, float inv) {
-  float y[4];
+// largest finite magnitude of a wave's values (infinities and NaN do not set a scale); inf: there are infinities
+template <int N>
+__device__ inline float kv8_amax(const float* x, bool* inf) {
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float v = x[i] * inv;
-    y[i] = v == v ? fminf(fmaxf(v, -448.f), 448.f) : v;
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));       // (ignores NaN)
+  m = wave_max(m);
+  *inf = m == INFINITY;
+  if (*inf) {                                  // uniform
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f);
+    m = wave_max(m);
   }
-  int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+  return m;
 }
+// four values / 2^e as e4m3 codes, nearest even (finite ones are at most 448 there, NaN stays NaN)
+__device__ inline uint32_t kv8_pack4(const float* x, float inv) {
+  int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, u, true);
+}
+// infinities to the largest magnitude of scale sc
+__device__ inline float kv8_saturate(float x, float sc) { return fabsf(x) == INFINITY ? copysignf(448.f * sc, x) : x; }
 __device__ inline void kv8_unpack4(uint32_t u, float scale, float* x) {
   x[0] = __builtin_amdgcn_cvt_f32_fp8(u, 0) * scale;
   x[1] = __builtin_amdgcn_cvt_f32_fp8(u, 1) * scale;
@@ -56,14 +64,128 @@ __device__ inline void kv8_unpack4(uint32_t u, float scale, float* x) {
   x[3] = __builtin_amdgcn_cvt_f32_fp8(u, 3) * scale;
 }
 
+// One group of one head, by a wave.  ph: its (page, head) block, part: the group
+// in it; lane t of src: the row of token t, -1 where it is not appended; tokens
+// below t0 are kept; row: the run's first.  FULL: all 16 tokens are appended.
+template <typename T, int DH, bool FULL>
+__device__ inline void append_keys(const Kv8AppendParams& p, size_t ph, int h, int part, int t0, int src, int row) {
+  constexpr int CL = DH / 4;                   // a lane: a quarter of a token's channels
+  const int lane = threadIdx.x & 63, t = lane >> 2, c0 = (lane & 3) * CL;
+  const int sr = FULL ? row + t : __shfl(src, t, 64);
+  uint4* dst = reinterpret_cast<uint4*>(p.c.k + (ph * PAGE + part * KV8_GROUP + t) * DH + c0);
+  float* scale = p.c.ks + ph * 4 + part;
+  // all loads in flight at once (a token that is not appended reads the run's first row, unused)
+  const T* k = reinterpret_cast<const T*>(p.k) + (size_t)(sr >= 0 ? sr : row) * p.ld_k + (size_t)h * DH + c0;
+  float x[CL], old = 1.f;
+  uint4 was[CL / 16];
+  if (!FULL && t0 > 0) {                       // uniform
+    old = *scale;
+#pragma unroll
+    for (int i = 0; i < CL / 16; ++i) was[i] = dst[i];
+  }
+#pragma unroll
+  for (int i = 0; i < CL; i += 16) Row16<T>::load(k + i, x + i);
+  if (!FULL && sr < 0) {
+#pragma unroll
+    for (int i = 0; i < CL; ++i) x[i] = 0.f;
+    if (t < t0) {
+#pragma unroll
+      for (int i = 0; i < CL; i += 16) {
+        kv8_unpack4(was[i / 16].x, old, x + i);
+        kv8_unpack4(was[i / 16].y, old, x + i + 4);
+        kv8_unpack4(was[i / 16].z, old, x + i + 8);
+        kv8_unpack4(was[i / 16].w, old, x + i + 12);
+      }
+    }
+  }
+  bool inf;
+  const int e = kv8_exponent(kv8_amax<CL>(x, &inf));
+  const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
+  if (inf) {
+#pragma unroll
+    for (int i = 0; i < CL; ++i) x[i] = kv8_saturate(x[i], sc);
+  }
+  if (FULL || sr >= 0 || (t < t0 && sc != old)) {
+#pragma unroll
+    for (int i = 0; i < CL; i += 16)
+      dst[i / 16] = make_uint4(kv8_pack4(x + i, inv), kv8_pack4(x + i + 4, inv), kv8_pack4(x + i + 8, inv),
+                               kv8_pack4(x + i + 12, inv));
+  }
+  if (lane == 0) *scale = sc;
+}
+
+template <typename T, int DH, bool FULL>
+__device__ inline void append_values(const Kv8AppendParams& p, size_t ph, int h, int part, int t0, int src, int row,
+                                     uint32_t fresh) {
+  constexpr int CL = DH / 64;                  // a lane: CL channels of all 16 tokens
+  const int c0 = (threadIdx.x & 63) * CL;
+  uint8_t* dst = p.c.v + (ph * DH + c0) * PAGE + part * KV8_GROUP;
+  float* scale = p.c.vs + ph * 4 + part;
+  T raw[KV8_GROUP][CL];
+  const T* v0 = reinterpret_cast<const T*>(p.v) + (size_t)h * DH + c0;
+#pragma unroll
+  for (int t = 0; t < KV8_GROUP; ++t) {
+    const int sr = FULL ? row + t : __builtin_amdgcn_readlane(src, t);
+    const T* v = v0 + (size_t)(sr >= 0 ? sr : row) * p.ld_v;
+    __builtin_memcpy(raw[t], __builtin_assume_aligned(v, CL * sizeof(T)), CL * sizeof(T));
+  }
+  float x[CL][KV8_GROUP], old = 1.f;
+  uint32_t was[CL][4];
+  if (!FULL) {
+    old = *scale;
+#pragma unroll
+    for (int c = 0; c < CL; ++c) {
+      const uint4 u = *reinterpret_cast<const uint4*>(dst + c * PAGE);
+      was[c][0] = u.x; was[c][1] = u.y; was[c][2] = u.z; was[c][3] = u.w;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CL; ++c)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float y[4];
+      if (!FULL) kv8_unpack4(was[c][q], old, y);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int t = 4 * q + b;
+        x[c][t] = TT<T>::ld(raw[t], c);
+        if (!FULL && !(fresh >> t & 1)) x[c][t] = t < t0 ? y[b] : 0.f;
+      }
+    }
+  bool inf;
+  const int e = kv8_exponent(kv8_amax<CL * KV8_GROUP>(&x[0][0], &inf));
+  const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
+  if (inf) {
+#pragma unroll
+    for (int i = 0; i < CL * KV8_GROUP; ++i) x[i / KV8_GROUP][i % KV8_GROUP] = kv8_saturate(x[i / KV8_GROUP][i % KV8_GROUP], sc);
+  }
+  const uint32_t live = fresh | ((1u << t0) - 1u);
+#pragma unroll
+  for (int c = 0; c < CL; ++c) {
+    uint32_t u[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      u[q] = kv8_pack4(&x[c][4 * q], inv);
+      if (!FULL) {
+        uint32_t keep = 0;                     // bytes of the tokens that stay as they were
+#pragma unroll
+        for (int b = 0; b < 4; ++b) keep |= (live >> (4 * q + b)) & 1u ? 0u : 0xFFu << (8 * b);
+        u[q] = (u[q] & ~keep) | (was[c][q] & keep);
+      }
+    }
+    *reinterpret_cast<uint4*>(dst + c * PAGE) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  if ((threadIdx.x & 63) == 0) *scale = sc;
+}
+
 template <typename T, int DH, int RC>
 __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
   static_assert(RC + 17 <= 64, "a lane per row of the window");
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool is_v = blockIdx.y & 1;
-  const int h = blockIdx.y >> 1;
-  const int r0 = (blockIdx.x * 4 + w) * RC;
+  const bool is_v = blockIdx.x & 1;            // units fastest: the heads of a row are read together
+  const int h = blockIdx.x >> 1;
+  const int r0 = (blockIdx.y * 4 + w) * RC;
   if (r0 >= p.rows) return;                    // uniform per wave
   // slots of rows r0 - 1 (lane 0) .. r0 + RC + 15
   const int row = r0 - 1 + lane;
@@ -76,126 +198,56 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
   const bool mine = lane >= 1 && lane <= RC;
   const bool follows = lane >= 1 && slot >= 0 && group == before;
   fault |= follows && slot <= sbefore;
-  if (blockIdx.y == 0 && __builtin_amdgcn_ballot_w64(mine && fault) != 0 && lane == 0) set_status(p.status, ST_BAD_SLOT);
+  if (blockIdx.x == 0 && __builtin_amdgcn_ballot_w64(mine && fault) != 0 && lane == 0) set_status(p.status, ST_BAD_SLOT);
   uint64_t leads = __builtin_amdgcn_ballot_w64(mine && slot >= 0 && !follows);
   while (leads) {                              // uniform
     const int ld = __builtin_ctzll(leads);
     leads &= leads - 1;
     const int s0 = __builtin_amdgcn_readlane(slot, ld), gr = s0 / KV8_GROUP, t0 = s0 % KV8_GROUP;
     // source row of each token of the group: lane t of src, -1: not appended
-    int src = -1, top = -1;
-#pragma unroll
-    for (int i = 0; i < KV8_GROUP; ++i) {
-      const int sl = ld + i < 64 ? __builtin_amdgcn_readlane(slot, (ld + i) & 63) : -1;
-      const int gi = ld + i < 64 ? __builtin_amdgcn_readlane(group, (ld + i) & 63) : -1;
-      if (gi != gr) break;
-      const int t = sl % KV8_GROUP;
-      if (t <= top) continue;                  // not ascending: skipped (status set above)
-      top = t;
-      if ((lane & 15) == t) src = r0 - 1 + ld + i;
+    int src;
+    const uint64_t line = __builtin_amdgcn_ballot_w64(slot == s0 + lane - ld && lane < ld + KV8_GROUP - t0) >> ld;
+    const int n = __builtin_ctzll(~line);      // rows of the run without a gap
+    if (ld + n < 64 && __builtin_amdgcn_readlane(group, (ld + n) & 63) == gr) {   // uniform: more of the group follow
+      int top = -1;
+      src = -1;
+      for (int i = 0; i < KV8_GROUP && ld + i < 64; ++i) {
+        const int sl = __builtin_amdgcn_readlane(slot, ld + i);
+        if (__builtin_amdgcn_readlane(group, ld + i) != gr) break;
+        const int t = sl % KV8_GROUP;
+        if (t <= top) continue;                // not ascending: skipped (status set above)
+        top = t;
+        if ((lane & 15) == t) src = r0 - 1 + ld + i;
+      }
+    } else {
+      const int t = lane & 15;
+      src = t >= t0 && t < t0 + n ? r0 - 1 + ld + t - t0 : -1;
     }
     const uint32_t fresh = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 16 && src >= 0);
     const int page = gr / 4, part = gr % 4;
     const size_t ph = (size_t)page * p.c.Hkv + h;
-    float* scale = (is_v ? p.c.vs : p.c.ks) + ph * 4 + part;
-    const float old = t0 > 0 ? *scale : 1.f;
-    if (!is_v) {
-      constexpr int CL = DH / 4;               // channels of a lane
-      const int t = lane >> 2, c0 = (lane & 3) * CL;
-      const int sr = __shfl(src, t, 64);
-      uint32_t* dst = reinterpret_cast<uint32_t*>(p.c.k + (ph * PAGE + part * KV8_GROUP + t) * DH + c0);
-      float x[CL];
-#pragma unroll
-      for (int i = 0; i < CL; ++i) x[i] = 0.f;
-      if (sr >= 0) {
-        const T* k = reinterpret_cast<const T*>(p.k) + (size_t)sr * p.ld_k + (size_t)h * DH + c0;
-#pragma unroll
-        for (int i = 0; i < CL; i += 16) Row16<T>::load(k + i, x + i);
-      } else if (t < t0) {
-#pragma unroll
-        for (int i = 0; i < CL; i += 16) {
-          const uint4 u = *reinterpret_cast<const uint4*>(dst + i / 4);
-          kv8_unpack4(u.x, old, x + i);
-          kv8_unpack4(u.y, old, x + i + 4);
-          kv8_unpack4(u.z, old, x + i + 8);
-          kv8_unpack4(u.w, old, x + i + 12);
-        }
-      }
-      float amax = 0.f;
-#pragma unroll
-      for (int i = 0; i < CL; ++i) amax = fmaxf(amax, kv8_finite_abs(x[i]));
-      const int e = kv8_exponent(wave_max(amax));
-      const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
-      if (sr >= 0 || (t < t0 && sc != old)) {
-#pragma unroll
-        for (int i = 0; i < CL; i += 16)
-          *reinterpret_cast<uint4*>(dst + i / 4) =
-              make_uint4(kv8_pack4(x + i, inv), kv8_pack4(x + i + 4, inv), kv8_pack4(x + i + 8, inv),
-                         kv8_pack4(x + i + 12, inv));
-      }
-      if (lane == 0) *scale = sc;
+    if (is_v) {
+      if (fresh == 0xFFFFu) append_values<T, DH, true>(p, ph, h, part, t0, src, r0 - 1 + ld, fresh);
+      else append_values<T, DH, false>(p, ph, h, part, t0, src, r0 - 1 + ld, fresh);
     } else {
-      constexpr int CL = DH / 64;
-      const int c0 = lane * CL;
-      uint8_t* dst = p.c.v + (ph * DH + c0) * PAGE + part * KV8_GROUP;
-      float x[CL][KV8_GROUP];
-      uint4 was[CL];
-      // every load in flight at once: a token that is not appended reads the run's first row, unused
-      T raw[KV8_GROUP][CL];
-#pragma unroll
-      for (int t = 0; t < KV8_GROUP; ++t) {
-        const int sr = __builtin_amdgcn_readlane(src, t);
-        const T* v = reinterpret_cast<const T*>(p.v) + (size_t)(sr >= 0 ? sr : r0 - 1 + ld) * p.ld_v + (size_t)h * DH + c0;
-        __builtin_memcpy(raw[t], __builtin_assume_aligned(v, CL * sizeof(T)), CL * sizeof(T));
-      }
-#pragma unroll
-      for (int c = 0; c < CL; ++c) {
-        was[c] = make_uint4(0, 0, 0, 0);
-        if (fresh != 0xFFFFu) was[c] = *reinterpret_cast<const uint4*>(dst + c * PAGE);   // uniform
-      }
-#pragma unroll
-      for (int t = 0; t < KV8_GROUP; ++t) {
-#pragma unroll
-        for (int c = 0; c < CL; ++c) {
-          const uint32_t u = t / 4 == 0 ? was[c].x : t / 4 == 1 ? was[c].y : t / 4 == 2 ? was[c].z : was[c].w;
-          float y[4];
-          kv8_unpack4(u, old, y);
-          x[c][t] = fresh >> t & 1 ? TT<T>::ld(raw[t], c) : t < t0 ? y[t & 3] : 0.f;
-        }
-      }
-      float amax = 0.f;
-#pragma unroll
-      for (int c = 0; c < CL; ++c)
-#pragma unroll
-        for (int t = 0; t < KV8_GROUP; ++t) amax = fmaxf(amax, kv8_finite_abs(x[c][t]));
-      const int e = kv8_exponent(wave_max(amax));
-      const float sc = kv8_pow2(e), inv = kv8_pow2(-e);
-      const uint32_t live = fresh | ((1u << t0) - 1u);
-#pragma unroll
-      for (int c = 0; c < CL; ++c) {
-        uint32_t u[4], o[4] = {was[c].x, was[c].y, was[c].z, was[c].w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t keep = 0;                   // bytes of the tokens that stay as they were
-#pragma unroll
-          for (int b = 0; b < 4; ++b) keep |= (live >> (4 * q + b)) & 1u ? 0u : 0xFFu << (8 * b);
-          u[q] = (kv8_pack4(&x[c][4 * q], inv) & ~keep) | (o[q] & keep);
-        }
-        *reinterpret_cast<uint4*>(dst + c * PAGE) = make_uint4(u[0], u[1], u[2], u[3]);
-      }
-      if (lane == 0) *scale = sc;
+      if (fresh == 0xFFFFu) append_keys<T, DH, true>(p, ph, h, part, t0, src, r0 - 1 + ld);
+      else append_keys<T, DH, false>(p, ph, h, part, t0, src, r0 - 1 + ld);
     }
   }
 }
+
+// Lanes find their rows' runs 16 to a wave where there are many (prompts: a run is
+// 16 rows; 15253 rows 36 us with 32, 29 with 16, 32 with 8), else one.
+constexpr int APPEND_RC = 16;
 
 template <typename T, int DH>
 static hipError_t launch_append_dh(const Kv8AppendParams& p, hipStream_t st) {
   // A round's rows spread over as many waves as there are rows; from a few
   // thousand rows on they are prompts, whose runs are 16 rows.
   if (p.rows <= 2048)
-    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 1>), dim3((p.rows + 3) / 4, 2 * p.c.Hkv), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 1>), dim3(2 * p.c.Hkv, (p.rows + 3) / 4), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 32>), dim3((p.rows + 127) / 128, 2 * p.c.Hkv), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((kv8_append_kernel<T, DH, APPEND_RC>), dim3(2 * p.c.Hkv, (p.rows + 4 * APPEND_RC - 1) / (4 * APPEND_RC)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
