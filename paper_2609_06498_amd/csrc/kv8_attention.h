@@ -10,10 +10,12 @@
 //     where its lane reads it; one barrier per page.
 // The PW states of a row tile are merged through LDS at the end.
 //
-// Per page a wave computes S^T = K Q^T (codes converted to bf16, exact; fp32
-// queries as three bf16 parts, so their 24 bits are all there) and O^T += V^T P^T
-// (codes converted to fp16, exact; probabilities rounded to fp16, fp32 rows as
-// two fp16 parts).  Tile row m of key tile kt is key 16 (m / 4) + 4 kt + m % 4, so
+// Per page a wave computes S^T = K Q^T and O^T += V^T P^T on the matrix cores.
+// Scores of bf16 queries: the key codes as they are against the query in two e4m3
+// parts (see Kv8Query); of fp32 queries: codes converted to bf16, exact, against
+// three bf16 parts, which hold all 24 bits.  Outputs: value
+// codes converted to fp16, exact, against probabilities rounded to fp16 (fp32
+// rows: two fp16 parts).  Tile row m of key tile kt is key 16 (m / 4) + 4 kt + m % 4, so
 // the lanes of group g = lane / 16 hold the scores of keys 16 g .. 16 g + 15:
 // one scale group.  With t = s ks + log2 vs (log2 units) the probability the
 // matrix cores take is 2^(t - M), the value scale included, and the row sum adds
@@ -82,7 +84,8 @@ struct Kv8Rows {
   }
 };
 __device__ __forceinline__ bool kv8_rows(const Kv8AttnParams& p, int s, Kv8Rows& r, int& bits) {
-  const int a = p.row_start[s], b = p.row_start[s + 1], len = p.kv_len[s];
+  const int a = __builtin_amdgcn_readfirstlane(p.row_start[s]), b = __builtin_amdgcn_readfirstlane(p.row_start[s + 1]);
+  const int len = __builtin_amdgcn_readfirstlane(p.kv_len[s]);
   bits = 0;
   if (a < 0 || b < a || b > p.rows) {
     bits = ST_CAPACITY;
@@ -106,26 +109,130 @@ __device__ __forceinline__ void kv8_store4(const Kv8AttnParams& p, int row, int 
   else frag_st4<T>(p.outf, row, c, y);
 }
 
-// a lane's eight query channels as bf16 parts (fp32: three, which hold its 24 bits)
-template <typename T, int NQ>
-__device__ __forceinline__ void kv8_query(const T* src, u32x4_t (&out)[NQ]) {
-  if constexpr (sizeof(T) == 2) {
-    out[0] = *(const gu4*)src;
-  } else {
-    float x[8];
-    Run4<float>::load(src, x);
-    Run4<float>::load(src + 4, x + 4);
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// A row group's queries (lane % 16's row, the channels that match the lane's key
+// runs: 64 c + 16 g + 0..15 of run c) and its scores against a key tile.
+//
+// fp32: three bf16 parts against the codes in bf16, in k steps of 32 channels.
+template <typename T, int DH>
+struct Kv8Query {
+  static constexpr int KI = DH / 64, NQ = 3;
+  u32x4_t part[2 * KI][NQ];
+  __device__ __forceinline__ float scale() const { return 1.f; }
+  __device__ __forceinline__ uint32_t anchor() const {   // a value that needs all loads
+    uint32_t a = 0;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+    for (int k = 0; k < 2 * KI; ++k) a |= part[k][0][0] | part[k][0][2];
+    return a;
+  }
+  __device__ __forceinline__ void load(const T* row) {
+    const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t u = f2bf2(x[2 * e], x[2 * e + 1]);
-        out[n][e] = u;
-        x[2 * e] -= bf2f(u & 0xFFFF);
-        x[2 * e + 1] -= bf2f(u >> 16);
+    for (int k = 0; k < 2 * KI; ++k) {
+      float x[8];
+      const T* src = row + (k >> 1) * 64 + g * 16 + (k & 1) * 8;
+      Run4<T>::load(src, x);
+      Run4<T>::load(src + 4, x + 4);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = f2bf2(x[2 * e], x[2 * e + 1]);
+          part[k][n][e] = u;
+          x[2 * e] -= bf2f(u & 0xFFFF);
+          x[2 * e + 1] -= bf2f(u >> 16);
+        }
+    }
+  }
+  template <int RG>
+  __device__ static __forceinline__ void scores(const Kv8Query (&q)[RG], const u32x4_t (&run)[KI], f32x4_t (&acc)[RG][4],
+                                                int kt) {
+#pragma unroll
+    for (int c = 0; c < KI; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4_t kf = h ? kv8_bf16(run[c][2], run[c][3]) : kv8_bf16(run[c][0], run[c][1]);
+#pragma unroll
+        for (int x = 0; x < RG; ++x)
+#pragma unroll
+          for (int n = NQ - 1; n >= 0; --n) acc[x][kt] = mma_frag(bf16(), kf, q[x].part[2 * c + h][n], acc[x][kt]);
       }
   }
-}
+};
+
+// bf16: q = 2^e (hi + lo) with hi, lo in e4m3 and the row's largest magnitude brought
+// to 224..448.  Eight significant bits are four and, signed, four more: exact for
+// elements down to 2^-10 of the row's largest, smaller ones are off by at most
+// 2^-18 of it (the subnormal step).  The key codes then go to the 128-deep e4m3
+// product as they were stored: no conversions, whose vector operations bound the
+// loop with bf16 operands (64 of 354 a page and wave), at the same matrix time.
+template <int DH>
+struct Kv8Query<bf16, DH> {
+  static constexpr int KI = DH / 64;
+  u32x4_t hi[KI], lo[KI];
+  float s;
+  __device__ __forceinline__ float scale() const { return s; }
+  __device__ __forceinline__ uint32_t anchor() const { return __float_as_uint(s); }   // (s needs all loads)
+  __device__ __forceinline__ void load(const bf16* row) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float x[KI][16], top = 0.f, a, b;
+#pragma unroll
+    for (int c = 0; c < KI; ++c) {
+      Row16<bf16>::load(row + c * 64 + g * 16, x[c]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[c][e]));
+    }
+    pair16(top, a, b);
+    pair32(fmaxf(a, b), a, b);
+    top = fmaxf(a, b);
+    int e = 0;                                 // top / 2^e in 224 .. 448 (exponents whose inverse is normal too)
+    if (top > 0.f && top < INFINITY) {
+      const float m = frexpf(top, &e);
+      e = min(max(e - 9 + (m > 0.875f ? 1 : 0), -126), 126);
+    }
+    s = __uint_as_float((uint32_t)(e + 127) << 23);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+    for (int c = 0; c < KI; ++c)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = x[c][4 * w + i] * inv;
+        int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+        hi[c][w] = (uint32_t)u;
+        y[0] -= __builtin_amdgcn_cvt_f32_fp8(u, 0);
+        y[1] -= __builtin_amdgcn_cvt_f32_fp8(u, 1);
+        y[2] -= __builtin_amdgcn_cvt_f32_fp8(u, 2);
+        y[3] -= __builtin_amdgcn_cvt_f32_fp8(u, 3);
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        lo[c][w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+      }
+  }
+  __device__ static __forceinline__ i32x8_t join(const u32x4_t& a, const u32x4_t& b) {
+    return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+  }
+  __device__ static __forceinline__ f32x4_t mma(const i32x8_t& a, const i32x8_t& b, f32x4_t acc) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, 0, 0, 0, 0);   // (scales of 0: none)
+  }
+  template <int RG>
+  __device__ static __forceinline__ void scores(const Kv8Query (&q)[RG], const u32x4_t (&run)[KI], f32x4_t (&acc)[RG][4],
+                                                int kt) {
+    if constexpr (KI == 1) {                   // 64 channels: both parts in one product
+      const i32x8_t k = join(run[0], run[0]);
+#pragma unroll
+      for (int x = 0; x < RG; ++x) acc[x][kt] = mma(k, join(q[x].lo[0], q[x].hi[0]), acc[x][kt]);
+    } else {
+      const i32x8_t k = join(run[0], run[1]);
+#pragma unroll
+      for (int x = 0; x < RG; ++x) acc[x][kt] = mma(k, join(q[x].lo[0], q[x].lo[1]), acc[x][kt]);
+#pragma unroll
+      for (int x = 0; x < RG; ++x) acc[x][kt] = mma(k, join(q[x].hi[0], q[x].hi[1]), acc[x][kt]);
+    }
+  }
+};
 
 // clears the bytes of the keys at or past lim_key of a lane's 16 (first key: key16)
 __device__ __forceinline__ u32x4_t kv8_clear_from(u32x4_t v, int key16, int lim_key) {
@@ -180,9 +287,8 @@ __device__ __forceinline__ void kv8_softmax(const f32x4_t (&sc)[4], int key16, i
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     t[e] = __builtin_amdgcn_exp2f(fmaf(t[e], c, ref));
-    sum += t[e];
+    if (NP > 1) sum += t[e];
   }
-  l = fmaf(sum, inv, l);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -192,13 +298,16 @@ __device__ __forceinline__ void kv8_softmax(const f32x4_t (&sc)[4], int key16, i
         float& u0 = t[8 * h + 2 * e];
         float& u1 = t[8 * h + 2 * e + 1];
         const uint32_t u = pk_f16(u0, u1);
+        const f16x2_t y = __builtin_bit_cast(f16x2_t, u);
         pa[h][n][e] = u;
+        // one part: the sum of the rounded values, two an operation, fp32
+        if (NP == 1) sum = __builtin_amdgcn_fdot2(y, f16x2_t{(_Float16)1.f, (_Float16)1.f}, sum, false);
         if (n + 1 < NP) {
-          const f16x2_t y = __builtin_bit_cast(f16x2_t, u);
           u0 -= (float)y[0];
           u1 -= (float)y[1];
         }
       }
+  l = fmaf(sum, inv, l);
 }
 
 // NaN values of an edge page: an output channel becomes NaN in the rows that see
@@ -403,11 +512,10 @@ __device__ __forceinline__ void kv8_finish(const Kv8AttnParams& p, const Kv8Spli
 // A wave's state, and one page against it: S^T = K Q^T, a softmax step, O^T += V^T P^T.
 template <typename T, int DH, int RG>
 struct Kv8Wave {
-  static constexpr int NQ = sizeof(T) == 2 ? 1 : 3;  // bf16 parts of a query
   static constexpr int NP = sizeof(T) == 2 ? 1 : 2;  // fp16 parts of a probability
-  static constexpr int KI = DH / 64, KS = 2 * KI;    // 16-byte runs per key row and lane, k steps
+  static constexpr int KI = DH / 64;                 // 16-byte runs per key row and lane
   static constexpr int DT = DH / 16;
-  u32x4_t qf[RG][KS][NQ];
+  Kv8Query<T, DH> q[RG];
   int lim[RG], lim_last;                       // keys that lane % 16's row sees, that the wave's last row sees
   float sl2;                                   // softmax scale, log2 units
   float M[RG], l[RG];
@@ -415,15 +523,12 @@ struct Kv8Wave {
 
   // rows from r0 on of the sequence's R (clamped rows are never stored)
   __device__ __forceinline__ void load(const Kv8AttnParams& p, const Kv8Rows& rows, int kvh, int G, int r0, int R) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
+    const int m16 = threadIdx.x & 15;
 #pragma unroll
     for (int i = 0; i < RG; ++i) {
       const int r = min(r0 + i * 16 + m16, R - 1), j = r / G;
       lim[i] = rows.limit(j, p.causal);
-      const T* q = reinterpret_cast<const T*>(p.q) + (size_t)(rows.start + j) * p.ld_q + (size_t)(kvh * G + r - j * G) * DH;
-#pragma unroll
-      for (int k = 0; k < KS; ++k)             // k step 2 c + h: channels 64 c + 16 g + 8 h ..
-        kv8_query<T, NQ>(q + (k >> 1) * 64 + g * 16 + (k & 1) * 8, qf[i][k]);
+      q[i].load(reinterpret_cast<const T*>(p.q) + (size_t)(rows.start + j) * p.ld_q + (size_t)(kvh * G + r - j * G) * DH);
       M[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
@@ -431,6 +536,11 @@ struct Kv8Wave {
     }
     lim_last = rows.limit((min(r0 + RG * 16, R) - 1) / G, p.causal);
     sl2 = p.scale * 1.4426950408889634f;
+  }
+
+  __device__ __forceinline__ void arrived() {  // (waits for the queries)
+#pragma unroll
+    for (int i = 0; i < RG; ++i) asm volatile("" ::"v"(M[i]), "v"(q[i].anchor()));
   }
 
   // Page with first key kp0.  kk, vrun(d): the lane's 16-byte runs; ksc, vsc: its
@@ -446,19 +556,7 @@ struct Kv8Wave {
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) sc[x][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-      for (int c = 0; c < KI; ++c) {
-        const u32x4_t u = kk[kt][c];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4_t kf = h ? kv8_bf16(u[2], u[3]) : kv8_bf16(u[0], u[1]);
-#pragma unroll
-          for (int x = 0; x < RG; ++x)
-#pragma unroll
-            for (int n = NQ - 1; n >= 0; --n) sc[x][kt] = mma_frag(bf16(), kf, qf[x][2 * c + h][n], sc[x][kt]);
-        }
-      }
+    for (int kt = 0; kt < 4; ++kt) Kv8Query<T, DH>::template scores<RG>(q, kk[kt], sc, kt);
     int lm[RG], ll = lim_last;
 #pragma unroll
     for (int x = 0; x < RG; ++x) lm[x] = lim[x];
@@ -478,7 +576,7 @@ struct Kv8Wave {
     __builtin_amdgcn_sched_barrier(0);
     u32x4_t pa[RG][2][NP];
 #pragma unroll
-    for (int x = 0; x < RG; ++x) kv8_softmax<DT, NP, EDGE>(sc[x], key16, lm[x], c, ev, inv, M[x], l[x], o[x], pa[x]);
+    for (int x = 0; x < RG; ++x) kv8_softmax<DT, NP, EDGE>(sc[x], key16, lm[x], c * q[x].scale(), ev, inv, M[x], l[x], o[x], pa[x]);
     uint32_t nan = 0;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
@@ -668,10 +766,7 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
   const bool own = r0 < it.R;                  // uniform: the wave has rows (else it only helps to load)
   w.load(p, it.rows, it.kvh, it.G, r0, it.R);
   const int lim_first = it.rows.limit(min(r0, it.R - 1) / it.G, p.causal);
-#pragma unroll
-  for (int x = 0; x < RG; ++x)
-#pragma unroll
-    for (int k = 0; k < W::KS; ++k) asm volatile("" ::"v"(w.qf[x][k][0]));   // the rows are in before the ring's loads are counted
+  w.arrived();                                 // the rows are in before the ring's loads are counted
   auto issue = [&](int i, uint32_t slot) {     // the wave's part of page i
     const size_t ph = (size_t)pages.take(p, it, i, pw, PW) * Hkv + it.kvh;
     const uint32_t l = lds0 + slot * SLOT;
