@@ -891,7 +891,9 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
 // kernel; more: as many row tiles of a workgroup's four waves as the rows fill,
 // the other waves on pages.  Pages per split: so that
 // the launch has about two workgroups per compute unit if every sequence reaches
-// key_cap, at least one page per page wave.  So a launch that splits has at most
+// key_cap, at least two pages per page wave (one sequence at
+// 4096 positions: 10.8 us a row, 15.8 a block; with one page 12.0 and 17.2, with
+// four 13.1 and 17.0).  So a launch that splits has at most
 // as many row tiles as compute units: KV8_COUNTERS bounds them.
 inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int cus) {
   const long long R = (long long)max_rows * (Hq / Hkv);
@@ -906,7 +908,7 @@ inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq
   const int pages = key_cap > 0 ? (key_cap + PAGE - 1) / PAGE : 1;
   const long long want = items < 2 * cus ? 2 * cus / items : 1;
   long long pp = (pages + want - 1) / want;
-  if (pp < sp.pw) pp = sp.pw;
+  if (pp < 2 * sp.pw) pp = 2 * sp.pw;
   sp.split_pages = (int)pp;
   sp.nsplit = (int)((pages + pp - 1) / pp);
   return sp;
