@@ -503,6 +503,18 @@ int dflow_kv8_attention(hipStream_t stream, int dtype, const dflow_kv8* cache, i
                         int max_len, int n_heads, const void* q, size_t ld_q, float scale, int causal, void* out,
                         size_t ld_out, void* workspace, size_t workspace_bytes, int32_t* status);
 
+/* A context whose target KV cache is held in 8 bits: dflow_create and
+ * dflow_workspace_bytes (on the current device) otherwise.  target: the cache of
+ * layer 0 (num_pages, kv heads and head_dim of the dims); each of its four arrays
+ * holds n_layers layers one after another, and cache->k_pool and v_pool are not
+ * used.  dflow_verify_block and the prefill calls append to it and attend over
+ * it; the drafter's context cache and every call's arguments and outputs are
+ * the same.  Half the cache bytes; keys and values carry e4m3's rounding (2^-4
+ * of each value at most). */
+size_t dflow_workspace_bytes_kv8(const dflow_dims* dims);
+int dflow_create_kv8(const dflow_dims* dims, const dflow_weights* w, const dflow_cache* cache, const dflow_kv8* target,
+                     void* workspace, size_t workspace_bytes, int32_t* status, hipStream_t stream, dflow_ctx** out);
+
 /* Kernel timing (tracing aid, not part of the method).  While enabled, every
  * weight-streaming GEMM launch and every attention launch is bracketed by HIP
  * events recorded on the launch's stream (up to 16384 launches between reads;

@@ -94,6 +94,13 @@ struct dflow_ctx {
   // between those calls, so prefill has captured states and features of its own.
   void *xf, *attnf, *actf, *uf;   // mmax rows (uf: the round's)
   void *hcapf, *ff;               // the round's rows
+  // 8-bit target cache (dflow_create_kv8): layer 0's pools, the rows' keys and
+  // values on their way to it, slots, row starts and lengths, attention partials
+  bool kv8 = false;
+  Kv8Cache k8{};
+  void *krows, *vrows;            // [mmax][kv_dim]
+  int *slot, *row_start, *kv_len; // [mmax], [max_batch + 1] (a prompt's segments: pairs), [max_batch + 1]
+  float* kv8_part;
   void *pre_hcapf, *pre_ff;       // a prefill chunk's rows
 
   // kernel timing record (dflow_profile)
@@ -170,7 +177,8 @@ int validate(const dflow_dims* d) {
 enum Buf {
   W_X, W_QKV, W_Q, W_HCAP, W_F, W_FPROJ, W_BG, W_PART_O, W_PART_ML, W_ROPE, W_AMAX, W_CARRY, W_TMP_POS, W_SSQ,
   W_AMAX_PART, W_COUNTERS, W_CTXKV, W_DKNORM, W_SAMP, W_SAMP_ROW, W_KPART, W_XF, W_ATTNF, W_ACTF, W_HCAPF,
-  W_UF, W_FF, W_RS, W_ARRIVE, W_PRE_HCAPF, W_PRE_FF, W_COUNT
+  W_UF, W_FF, W_RS, W_ARRIVE, W_PRE_HCAPF, W_PRE_FF, W_KROWS, W_VROWS, W_SLOT, W_ROW_START, W_KV_LEN, W_KV8_PART,
+  W_COUNT
 };
 struct Layout {
   size_t off[W_COUNT];
@@ -178,7 +186,9 @@ struct Layout {
 };
 
 // Workspace carve-up; identical for dflow_workspace_bytes and dflow_create.
-Layout plan(const dflow_dims* d, int* nsplit_out, int* lm_groups_out) {
+// kv8_cus: the compute units of the device for a context with an 8-bit target
+// cache (its attention is split by them), else 0.
+Layout plan(const dflow_dims* d, int* nsplit_out, int* lm_groups_out, int kv8_cus = 0) {
   const size_t elt = d->dtype == DFLOW_BF16 ? 2 : 4;
   const int qd = d->n_heads * d->head_dim, kvd = d->n_kv_heads * d->head_dim;
   const int qkvn = qd + 2 * kvd;
@@ -249,6 +259,22 @@ Layout plan(const dflow_dims* d, int* nsplit_out, int* lm_groups_out) {
     add(W_PRE_HCAPF, pre_fr * d->n_capture * d->d);
     add(W_PRE_FF, pre_fr * d->d);
   }
+  if (kv8_cus > 0) {   // 8-bit target cache
+    const int cap = d->max_pages * PAGE;
+    const bool bf = d->dtype == DFLOW_BF16;
+    add(W_KROWS, (size_t)mmax * kvd * elt);
+    add(W_VROWS, (size_t)mmax * kvd * elt);
+    add(W_SLOT, (size_t)mmax * 4);
+    add(W_ROW_START, (size_t)2 * (d->max_batch + 1) * 4);
+    add(W_KV_LEN, (size_t)(d->max_batch + 1) * 4);
+    size_t part = KV8_COUNTERS * 4;
+    const size_t r = kv8_attn_workspace(bf, d->max_batch, d->block, cap, d->n_heads, d->n_kv_heads, d->head_dim, kv8_cus,
+                                        false);
+    const size_t q = kv8_attn_workspace(bf, 1, d->max_rows, cap, d->n_heads, d->n_kv_heads, d->head_dim, kv8_cus, true);
+    if (r > part) part = r;
+    if (q > part) part = q;
+    add(W_KV8_PART, part);
+  }
   L.total = o;
   if (nsplit_out) *nsplit_out = nsplit;
   if (lm_groups_out) *lm_groups_out = lm_groups;
@@ -262,23 +288,58 @@ extern "C" size_t dflow_workspace_bytes(const dflow_dims* dims) {
   return plan(dims, nullptr, nullptr).total;
 }
 
+namespace {
+int device_cus(int* cus);
+int kv8_cache(const char* who, const dflow_kv8* k, Kv8Cache* c);
+int create(const dflow_dims* dims, const dflow_weights* w, const dflow_cache* cache, const dflow_kv8* kv8,
+           void* workspace, size_t workspace_bytes, int32_t* status, hipStream_t stream, dflow_ctx** out);
+}  // namespace
+
+extern "C" size_t dflow_workspace_bytes_kv8(const dflow_dims* dims) {
+  int cus = 0;
+  if (validate(dims) != DFLOW_OK || device_cus(&cus) != DFLOW_OK) return 0;
+  return plan(dims, nullptr, nullptr, cus).total;
+}
+
 extern "C" int dflow_create(const dflow_dims* dims, const dflow_weights* w, const dflow_cache* cache,
                             void* workspace, size_t workspace_bytes, int32_t* status, hipStream_t stream,
                             dflow_ctx** out) {
+  return create(dims, w, cache, nullptr, workspace, workspace_bytes, status, stream, out);
+}
+
+extern "C" int dflow_create_kv8(const dflow_dims* dims, const dflow_weights* w, const dflow_cache* cache,
+                                const dflow_kv8* target, void* workspace, size_t workspace_bytes, int32_t* status,
+                                hipStream_t stream, dflow_ctx** out) {
+  if (!target) return fail(DFLOW_EINVAL, "create_kv8: null target cache");
+  return create(dims, w, cache, target, workspace, workspace_bytes, status, stream, out);
+}
+
+namespace {
+int create(const dflow_dims* dims, const dflow_weights* w, const dflow_cache* cache, const dflow_kv8* kv8,
+           void* workspace, size_t workspace_bytes, int32_t* status, hipStream_t stream, dflow_ctx** out) {
   int rc = validate(dims);
   if (rc) return rc;
+  Kv8Cache k8{};
+  int cus8 = 0;
+  if (kv8) {
+    if ((rc = kv8_cache("create_kv8", kv8, &k8))) return rc;
+    if (k8.num_pages != dims->num_pages || k8.Hkv != dims->n_kv_heads || k8.Dh != dims->head_dim)
+      return fail(DFLOW_ESHAPE, "create_kv8: cache of %d pages, %d kv heads, head_dim %d; dims have %d, %d, %d",
+                  k8.num_pages, k8.Hkv, k8.Dh, dims->num_pages, dims->n_kv_heads, dims->head_dim);
+    if ((rc = device_cus(&cus8))) return rc;
+  }
   if (!w || !cache || !out || !workspace || !status) return fail(DFLOW_EINVAL, "create: null argument");
   if (((uintptr_t)workspace & 255) || ((uintptr_t)status & 3))
     return fail(DFLOW_EINVAL, "create: workspace must be 256-byte and status 4-byte aligned");
   {
-    const size_t need = plan(dims, nullptr, nullptr).total;
+    const size_t need = plan(dims, nullptr, nullptr, cus8).total;
     if (workspace_bytes < need)
       return fail(DFLOW_ECAPACITY, "create: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   }
   const void* req[] = {w->embed, w->lm_head, w->layers, w->draft_layers, w->draft_lm_head, w->draft_wkv_ctx,
                        w->e_mask, w->w_c, w->g_c, w->relay_w1, w->relay_c1, w->relay_w2, w->relay_c2,
-                       w->relay_ln_g, w->relay_ln_b, cache->k_pool, cache->v_pool, cache->ck_pool, cache->cv_pool,
-                       cache->page_table};
+                       w->relay_ln_g, w->relay_ln_b, cache->ck_pool, cache->cv_pool, cache->page_table,
+                       kv8 ? kv8->k : cache->k_pool, kv8 ? kv8->v : cache->v_pool};
   for (size_t i = 0; i < sizeof(req) / sizeof(req[0]); ++i)
     if (!req[i]) return fail(DFLOW_EINVAL, "create: required pointer #%zu is null", i);
   auto chk_layer = [](const dflow_layer& L) {
@@ -319,7 +380,9 @@ extern "C" int dflow_create(const dflow_dims* dims, const dflow_weights* w, cons
   c->c = *cache;
   c->pool_layer_elems = (size_t)dims->num_pages * dims->n_kv_heads * PAGE * dims->head_dim;
 
-  Layout L = plan(dims, &c->nsplit, &c->lm_groups);
+  c->kv8 = kv8 != nullptr;
+  c->k8 = k8;
+  Layout L = plan(dims, &c->nsplit, &c->lm_groups, cus8);
   c->split_keys = split_keys_for(c->bf, dims->max_batch, dims->n_kv_heads, dims->max_pages * PAGE);
   c->round_chunks = round_chunks_for(dims->max_batch, dims->n_kv_heads, dims->max_pages * PAGE, c->split_keys, c->cus);
   c->ws = workspace;
@@ -357,6 +420,14 @@ extern "C" int dflow_create(const dflow_dims* dims, const dflow_weights* w, cons
   c->arrive = (unsigned*)(b + L.off[W_ARRIVE]);
   c->pre_hcapf = b + L.off[W_PRE_HCAPF];
   c->pre_ff = b + L.off[W_PRE_FF];
+  if (c->kv8) {
+    c->krows = b + L.off[W_KROWS];
+    c->vrows = b + L.off[W_VROWS];
+    c->slot = (int*)(b + L.off[W_SLOT]);
+    c->row_start = (int*)(b + L.off[W_ROW_START]);
+    c->kv_len = (int*)(b + L.off[W_KV_LEN]);
+    c->kv8_part = (float*)(b + L.off[W_KV8_PART]);
+  }
 
   // RoPE table: angle p * theta^(-2i/Dh) evaluated in double
   const int half = dims->head_dim / 2;
@@ -396,6 +467,7 @@ extern "C" int dflow_create(const dflow_dims* dims, const dflow_weights* w, cons
   *out = c;
   return DFLOW_OK;
 }
+}  // namespace
 
 extern "C" int dflow_destroy(dflow_ctx* c) {
   if (!c) return fail(DFLOW_EINVAL, "destroy: null context");
@@ -589,12 +661,90 @@ RopeParams rope_params(dflow_ctx* c, const dflow_layer& L, int nseq, int Bq, int
   return r;
 }
 
-// One Qwen3-style decoder layer over x (M = nseq*Bq rows) in place.  Prefill:
+// Keys and values of `rows` rows from row0 on to the 8-bit cache of target layer
+// `l`, and the attention of their queries over it: a round's nseq sequences of Bq
+// rows, or one segment of a prompt chunk (seg; its row starts at 2 seg_i).
+hipError_t kv8_attend(dflow_ctx* c, hipStream_t st, int l, int nseq, int Bq, const int* page_table, const Seg* seg,
+                      int seg_i) {
+  const size_t layer = (size_t)c->k8.num_pages * c->k8.Hkv, codes = layer * PAGE * c->k8.Dh * l, scales = layer * 4 * l;
+  Kv8Cache k8 = c->k8;
+  k8.k += codes;
+  k8.v += codes;
+  k8.ks += scales;
+  k8.vs += scales;
+  const int row0 = seg ? seg->row0 : 0, rows = seg ? seg->n : nseq * Bq;
+  Kv8AppendParams a{};
+  a.c = k8;
+  a.k = (char*)c->krows + (size_t)row0 * c->kv_dim * c->elt;
+  a.v = (char*)c->vrows + (size_t)row0 * c->kv_dim * c->elt;
+  a.ld_k = a.ld_v = c->kv_dim;
+  a.slot = c->slot + row0;
+  a.rows = rows;
+  a.status = c->status;
+  hipError_t e = launch_kv8_append(c->bf, a, st);
+  if (e != hipSuccess) return e;
+  Kv8AttnParams p{};
+  p.c = k8;
+  p.page_table = page_table;
+  p.kv_len = c->kv_len + (seg ? seg_i : 0);
+  p.row_start = c->row_start + (seg ? 2 * seg_i : 0);
+  p.q = c->q;
+  p.outf = fout(c, c->attnf, c->q_dim);
+  p.ld_q = c->q_dim;
+  p.scale = 1.0f / std::sqrt((float)c->dm.head_dim);
+  p.nseq = seg ? 1 : nseq;
+  p.rows = row0 + rows;
+  p.max_rows = seg ? seg->n : Bq;
+  p.Hq = c->dm.n_heads;
+  p.max_pages = c->dm.max_pages;
+  // a prompt's length is the host's: splits behind it are not launched
+  p.key_cap = seg ? seg->pos0 + seg->n : c->dm.max_pages * PAGE;
+  p.causal = 1;
+  p.plan_seq = seg ? 1 : c->dm.max_batch;
+  p.prompt = seg ? 1 : 0;
+  p.cus = c->cus;
+  p.part = c->kv8_part;
+  p.status = c->status;
+  const bool rec = c->prof && c->n_ev < PROF_MAX;
+  if (rec && (e = hipEventRecord(c->ev0[c->n_ev], st)) != hipSuccess) return e;
+  if ((e = launch_kv8_attention(c->bf, p, st)) != hipSuccess) return e;
+  if (rec) {
+    if ((e = hipEventRecord(c->ev1[c->n_ev], st)) != hipSuccess) return e;
+    c->ev_rec[c->n_ev++] = {CLS_ATTN, 0, 0, rows, c->phase, 0.0};
+  }
+  return hipSuccess;
+}
+
+// Slots, row starts and lengths of the rows that the next target layers process.
+hipError_t kv8_rows(dflow_ctx* c, hipStream_t st, int nseq, int Bq, const int* start_pos, const int* page_table,
+                    const std::vector<Seg>* segs) {
+  Kv8BatchParams b{};
+  b.max_pages = c->dm.max_pages;
+  b.num_pages = c->dm.num_pages;
+  b.status = c->status;
+  for (size_t i = 0; i < (segs ? segs->size() : 1); ++i) {
+    const Seg* sg = segs ? &(*segs)[i] : nullptr;
+    b.nseq = sg ? 1 : nseq;
+    b.B = sg ? sg->n : Bq;
+    b.start_pos = sg ? c->tmp_pos + sg->seq : start_pos;
+    b.page_table = sg ? c->c.page_table + (size_t)sg->seq * c->dm.max_pages : page_table;
+    b.row0 = sg ? sg->row0 : 0;
+    b.slot = c->slot + b.row0;
+    b.row_start = c->row_start + (sg ? 2 * i : 0);
+    b.kv_len = c->kv_len + (sg ? i : 0);
+    const hipError_t e = launch_kv8_batch(b, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// One Qwen3-style decoder layer over x (M = nseq*Bq rows) in place; kv8 >= 0: the
+// target layer whose 8-bit cache takes the place of kpool and vpool.  Prefill:
 // nseq = 1, Bq = the chunk's rows and their segments; a segment's position is
 // in c->tmp_pos[seq].
 hipError_t decoder_layer(dflow_ctx* c, hipStream_t st, const dflow_layer& L, int nseq, int Bq, const int* start_pos,
                          const int* page_table, void* kpool, void* vpool, int causal, void* capture,
-                         FragOut capf = FragOut{nullptr, 0, 0}, const std::vector<Seg>* segs = nullptr) {
+                         FragOut capf = FragOut{nullptr, 0, 0}, const std::vector<Seg>* segs = nullptr, int kv8 = -1) {
   const dflow_dims& d = c->dm;
   const int M = nseq * Bq;
   hipError_t e;
@@ -624,7 +774,7 @@ hipError_t decoder_layer(dflow_ctx* c, hipStream_t st, const dflow_layer& L, int
   if ((e = gemm(c, st, EPI_STORE_F32, c->x, d.d, L.wqkv, M, c->qkv_n, d.d, c->qkv, c->qkv_n, nullptr, 0, nullptr, 0,
                 nullptr, nullptr, 0, attn_n, nullptr, c->qkv_ks, fq)))
     return e;
-  const bool fused = !segs && attention_fuses_rope(c->bf, Bq, c->G, d.head_dim, c->split_keys);
+  const bool fused = !segs && kv8 < 0 && attention_fuses_rope(c->bf, Bq, c->G, d.head_dim, c->split_keys);
   for (size_t i = 0; i < (segs ? segs->size() : 1); ++i) {
     const Seg* sg = segs ? &(*segs)[i] : nullptr;
     const int rows = sg ? sg->n : Bq;
@@ -636,7 +786,16 @@ hipError_t decoder_layer(dflow_ctx* c, hipStream_t st, const dflow_layer& L, int
       if (sg) r.q_out = (char*)c->q + (size_t)sg->row0 * c->q_dim * c->elt;
       r.ld = c->qkv_n;
       r.part = c->qkv_ks == 2 ? (size_t)M * c->qkv_n : 0;
+      if (kv8 >= 0) {
+        const size_t at = (size_t)(sg ? sg->row0 : 0) * c->kv_dim * c->elt;
+        r.k_rows = (char*)c->krows + at;
+        r.v_rows = (char*)c->vrows + at;
+      }
       if ((e = launch_qk_rope_write(c->bf, r, st))) return e;
+    }
+    if (kv8 >= 0) {
+      if ((e = kv8_attend(c, st, kv8, nseq, Bq, pt, sg, (int)i))) return e;
+      continue;
     }
     if ((e = attention(c, st, L, nseq, rows, pos, pt, kpool, vpool, causal, fused, sg))) return e;
   }
@@ -660,6 +819,7 @@ hipError_t target_layers(dflow_ctx* c, hipStream_t st, int nseq, int Bq, const i
                          const int* page_table, bool rows_out, const std::vector<Seg>* segs) {
   const dflow_dims& d = c->dm;
   hipError_t e;
+  if (c->kv8 && (e = kv8_rows(c, st, nseq, Bq, start_pos, page_table, segs))) return e;
   int ci = 0;
   for (int l = 0; l < d.n_layers; ++l) {
     void* cap = nullptr;
@@ -669,8 +829,10 @@ hipError_t target_layers(dflow_ctx* c, hipStream_t st, int nseq, int Bq, const i
       if (rows_out) cap = (char*)c->hcap + (size_t)ci * d.d * c->elt;
       ++ci;
     }
-    if ((e = decoder_layer(c, st, c->layers[l], nseq, Bq, start_pos, page_table, pool_layer(c, c->c.k_pool, l),
-                           pool_layer(c, c->c.v_pool, l), 1, cap, capf, segs)))
+    if ((e = c->kv8 ? decoder_layer(c, st, c->layers[l], nseq, Bq, start_pos, page_table, nullptr, nullptr, 1, cap, capf,
+                                    segs, l)
+                    : decoder_layer(c, st, c->layers[l], nseq, Bq, start_pos, page_table, pool_layer(c, c->c.k_pool, l),
+                                    pool_layer(c, c->c.v_pool, l), 1, cap, capf, segs)))
       return e;
   }
   return hipSuccess;
@@ -1142,7 +1304,7 @@ extern "C" size_t dflow_kv8_attention_workspace(int dtype, int nseq, int max_row
   }
   if (device_cus(&cus)) return (size_t)-1;
   return max_rows < 1 ? 0 : kv8_attn_workspace(dtype == DFLOW_BF16, nseq, max_rows, max_len, n_heads, n_kv_heads,
-                                               head_dim, cus);
+                                               head_dim, cus, false);
 }
 
 extern "C" int dflow_kv8_attention(hipStream_t st, int dtype, const dflow_kv8* cache, int nseq, const int32_t* page_table,
@@ -1164,7 +1326,7 @@ extern "C" int dflow_kv8_attention(hipStream_t st, int dtype, const dflow_kv8* c
   if ((rc = kv8_rows_arg("kv8_attention", "out", dtype, out, ld_out, width))) return rc;
   if ((rc = device_cus(&p.cus))) return rc;
   p.key_cap = (long long)max_len < (long long)max_pages * PAGE ? max_len : max_pages * PAGE;
-  const size_t need = kv8_attn_workspace(dtype == DFLOW_BF16, nseq, max_rows, p.key_cap, n_heads, p.c.Hkv, p.c.Dh, p.cus);
+  const size_t need = kv8_attn_workspace(dtype == DFLOW_BF16, nseq, max_rows, p.key_cap, n_heads, p.c.Hkv, p.c.Dh, p.cus, false);
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 15)))
     return fail(DFLOW_EINVAL, "kv8_attention: workspace must be given and 16-byte aligned");
   if (workspace_bytes < need)
@@ -1183,6 +1345,7 @@ extern "C" int dflow_kv8_attention(hipStream_t st, int dtype, const dflow_kv8* c
   p.Hq = n_heads;
   p.max_pages = max_pages;
   p.causal = causal != 0;
+  p.plan_seq = nseq;
   p.part = (float*)workspace;
   p.status = status;
   HIPCHK(launch_kv8_attention(dtype == DFLOW_BF16, p, st));

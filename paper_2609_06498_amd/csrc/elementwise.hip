@@ -189,13 +189,19 @@ __global__ void __launch_bounds__(256) qk_rope_kernel(RopeParams p) {
     }
   }
   size_t page_base = 0;
-  if (!is_q) {
+  if (!is_q && !p.k_rows) {
     const int page = p.page_table[(size_t)s * p.max_pages + pidx];
     if (page < 0 || page >= p.num_pages) {
       if (c == 0) set_status(p.status, ST_BAD_PAGE);
       return;
     }
     page_base = (size_t)layer * p.pool_stride + ((size_t)page * p.Hkv + kvh) * PAGE * DH;
+  }
+  const size_t row_off = ((size_t)row * p.Hkv + kvh) * DH + c;   // of k_rows and v_rows
+  if (!is_q && !is_k && p.v_rows) {
+    Run4<T>::store(reinterpret_cast<T*>(p.v_rows) + row_off, x[0]);
+    Run4<T>::store(reinterpret_cast<T*>(p.v_rows) + row_off + HALF, x[1]);
+    return;
   }
   if (!is_q && !is_k) {        // value head, fragment order (see kernels.h)
     T* vp = reinterpret_cast<T*>(p.vpool) + page_base;
@@ -241,6 +247,9 @@ __global__ void __launch_bounds__(256) qk_rope_kernel(RopeParams p) {
     T* q = reinterpret_cast<T*>(p.q_out) + (size_t)row * p.nq * DH + (size_t)h * DH + c;
     Run4<T>::store(q, o1);
     Run4<T>::store(q + HALF, o2);
+  } else if (p.k_rows) {
+    Run4<T>::store(reinterpret_cast<T*>(p.k_rows) + row_off, o1);
+    Run4<T>::store(reinterpret_cast<T*>(p.k_rows) + row_off + HALF, o2);
   } else {
     // key elements d .. d + 3 of this slot are one run in fragment order (see kernels.h)
     auto koff = [&](int d) -> size_t {

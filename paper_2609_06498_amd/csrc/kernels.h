@@ -87,6 +87,7 @@ struct RopeParams {
   const int* row_limit;           // nullable [nseq]: only rows j <= row_limit[s] are written
   void* q_out;                    // [M, nq*Dh]
   void* kpool; void* vpool;       // this layer's pools
+  void* k_rows; void* v_rows;     // set: keys and values go here, [M, Hkv*Dh], and no pool is written
   const int* page_table; int max_pages; int num_pages;
   int* status;
   float eps;

@@ -53,13 +53,29 @@ struct Kv8AttnParams {
   int Hq, max_pages;
   int key_cap;               // keys read at most: min(max_len, 64 max_pages)
   int causal;
+  // Work split: planned for plan_seq sequences; prompt: in a prefill, whose splits
+  // (32 pages) and tiles do not depend on the chunk, so neither does a row's result
+  int plan_seq, prompt;
   int cus;
   float* part;               // arrival counters and split partials, kv8_attn_workspace bytes
   int* status;
 };
 constexpr int KV8_COUNTERS = 1024;   // 4-byte arrival counters at the start of the workspace, zero between calls
-size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus);
+size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus, bool prompt);
 hipError_t launch_kv8_attention(bool bf16, const Kv8AttnParams& p, hipStream_t s);
+
+// Slots, row starts and lengths of nseq sequences of B rows at start_pos[s] .. (rows
+// without a page in the table: slot -1, status).  row_start [nseq + 1], kv_len [nseq].
+struct Kv8BatchParams {
+  int nseq, B;
+  const int* start_pos;
+  const int* page_table;
+  int max_pages, num_pages;
+  int row0;                  // first row of the call's rows
+  int *slot, *row_start, *kv_len;
+  int* status;
+};
+hipError_t launch_kv8_batch(const Kv8BatchParams& p, hipStream_t s);
 
 constexpr int PAGES_MAX_SEQ = 1024;
 struct PageResizeParams {

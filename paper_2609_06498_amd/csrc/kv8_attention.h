@@ -889,18 +889,19 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
 
 // Work split, a function of the host's arguments only.  One row group: the direct
 // kernel; more: as many row tiles of a workgroup's four waves as the rows fill,
-// the other waves on pages.  Pages per split: so that
-// the launch has about two workgroups per compute unit if every sequence reaches
-// key_cap, at least two pages per page wave (one sequence at
-// 4096 positions: 10.8 us a row, 15.8 a block; with one page 12.0 and 17.2, with
-// four 13.1 and 17.0).  So a launch that splits has at most
-// as many row tiles as compute units: KV8_COUNTERS bounds them.
-inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int cus) {
+// the other waves on pages.  Pages per split: so that the launch has about two
+// workgroups per compute unit if every sequence reaches key_cap, at least two pages
+// per page wave (one sequence at 4096 positions: 10.8 us a row, 15.8 a block; with
+// one page 12.0 and 17.2, with four 13.1 and 17.0).  So a launch that splits has at
+// most as many row tiles as compute units: KV8_COUNTERS bounds them.  A prompt's
+// chunks all take the tiles of many rows and splits of KV8_PROMPT_PAGES pages.
+constexpr int KV8_PROMPT_PAGES = 32;
+inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int cus, bool prompt) {
   const long long R = (long long)max_rows * (Hq / Hkv);
   Kv8Split sp;
-  sp.rg = bf16 && R > 32 ? 2 : 1;
+  sp.rg = bf16 && (R > 32 || prompt) ? 2 : 1;
   const int per = 16 * sp.rg;
-  sp.tw = R <= per ? 1 : (R <= 2 * per ? 2 : 4);
+  sp.tw = prompt ? 4 : (R <= per ? 1 : (R <= 2 * per ? 2 : 4));
   sp.pw = 4 / sp.tw;
   sp.tiles = (int)((R + per * sp.tw - 1) / (per * sp.tw));
   if (cus > KV8_COUNTERS) cus = KV8_COUNTERS;
@@ -909,6 +910,7 @@ inline Kv8Split kv8_split(bool bf16, int nseq, int max_rows, int key_cap, int Hq
   const long long want = items < 2 * cus ? 2 * cus / items : 1;
   long long pp = (pages + want - 1) / want;
   if (pp < 2 * sp.pw) pp = 2 * sp.pw;
+  if (prompt) pp = KV8_PROMPT_PAGES;
   sp.split_pages = (int)pp;
   sp.nsplit = (int)((pages + pp - 1) / pp);
   return sp;
@@ -962,13 +964,14 @@ static hipError_t launch_kv8_dh(const Kv8AttnParams& p, const Kv8Split& sp, hipS
   return launch_kv8_direct<T, DH>(p, sp, st);
 }
 
-size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus) {
-  return kv8_part_floats(kv8_split(bf16, nseq, max_rows, key_cap, Hq, Hkv, cus), nseq, Hkv, Dh) * sizeof(float);
+size_t kv8_attn_workspace(bool bf16, int nseq, int max_rows, int key_cap, int Hq, int Hkv, int Dh, int cus,
+                          bool prompt) {
+  return kv8_part_floats(kv8_split(bf16, nseq, max_rows, key_cap, Hq, Hkv, cus, prompt), nseq, Hkv, Dh) * sizeof(float);
 }
 
 hipError_t launch_kv8_attention(bool bf16, const Kv8AttnParams& p, hipStream_t st) {
   if (p.nseq < 1 || p.rows < 1 || p.max_rows < 1) return hipSuccess;
-  const Kv8Split sp = kv8_split(bf16, p.nseq, p.max_rows, p.key_cap, p.Hq, p.c.Hkv, p.cus);
+  const Kv8Split sp = kv8_split(bf16, p.plan_seq, p.max_rows, p.key_cap, p.Hq, p.c.Hkv, p.cus, p.prompt != 0);
   if (p.c.Dh == 128)
     return bf16 ? launch_kv8_dh<dflow::bf16, 128>(p, sp, st) : launch_kv8_dh<float, 128>(p, sp, st);
   if (p.c.Dh == 64)

@@ -258,6 +258,32 @@ hipError_t launch_kv8_append(bool isbf, const Kv8AppendParams& p, hipStream_t st
   return hipErrorInvalidValue;
 }
 
+// ---------------------------------------------------------------- rows of a round
+__global__ void __launch_bounds__(256) kv8_batch_kernel(Kv8BatchParams p) {
+  const int i = blockIdx.x * 256 + threadIdx.x, rows = p.nseq * p.B;
+  if (i <= p.nseq) {
+    p.row_start[i] = p.row0 + i * p.B;
+    if (i < p.nseq) p.kv_len[i] = p.start_pos[i] + p.B;
+  }
+  if (i >= rows) return;
+  const int s = i / p.B, pos = p.start_pos[s] + i - s * p.B;
+  int slot = -1;
+  if (pos < 0 || pos / PAGE >= p.max_pages) {
+    set_status(p.status, ST_CAPACITY);
+  } else {
+    const int page = p.page_table[(size_t)s * p.max_pages + pos / PAGE];
+    if (page < 0 || page >= p.num_pages) set_status(p.status, ST_BAD_PAGE);
+    else slot = page * PAGE + pos % PAGE;
+  }
+  p.slot[i] = slot;
+}
+
+hipError_t launch_kv8_batch(const Kv8BatchParams& p, hipStream_t st) {
+  const int n = p.nseq * p.B > p.nseq ? p.nseq * p.B : p.nseq + 1;
+  hipLaunchKernelGGL(kv8_batch_kernel, dim3((n + 255) / 256), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- pages
 // Rows of a page table resized to request lengths.  One workgroup, a thread per
 // sequence: target = ceil((len + new) / 64) pages; the pages above it go back to

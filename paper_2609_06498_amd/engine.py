@@ -20,6 +20,12 @@ accept_sampled -> kv_commit.  Each request draws from its own Philox stream
 (its request id under the engine's sampling seed), so its tokens do not
 depend on its slot or on the requests that share its rounds.
 
+With a runtime whose page table has a pool (Runtime num_pages), slots own the
+pages their tokens need instead of a full row each: rows grow on the device
+before every prefill and round (dflow_page_resize) and a finished request's pages go
+back to the pool.  A request is admitted once the pool can hold the longest it may
+become beside those of the active requests, so rows never run out.
+
 Every step runs in the library's kernels; this layer only sequences calls
 and keeps the per-request bookkeeping.  The one host synchronisation per
 round reads the committed tokens, which the retirement decision needs.
@@ -74,6 +80,10 @@ class Engine:
         self.seq_len, self.anchor = i32(n), i32(n)
         self.draft_tok, self.block, self.tgt = i32(n, B - 1), i32(n, B), i32(n, B)
         self.accept, self.committed, self.n_carry = i32(n), i32(n, B), i32(n)
+        self.pool = getattr(rt, "page_pool", None)
+        if self.pool is not None:
+            self.block_len = torch.full((n,), B, dtype=torch.int32, device=dev)
+            self.free_pages = rt.num_pages            # beyond what active requests may come to need
         self.force_mean = force_mean
         self.seed = seed
         self.temperature = temperature
@@ -105,6 +115,9 @@ class Engine:
         if prompt.size + max_new + self.B > self.capacity:
             raise DFlowError(f"prompt {prompt.size} + {max_new} new tokens exceed the context capacity "
                              f"{self.capacity - self.B}")
+        if self.pool is not None and self._pages(prompt.size, max_new) > self.rt.num_pages:
+            raise DFlowError(f"prompt {prompt.size} + {max_new} new tokens need more than the pool's "
+                             f"{self.rt.num_pages} pages")
         if (self.force_mean is None) != (traj is None):
             raise DFlowError("forcing needs a trajectory per request and an engine built with force_mean")
         if traj is not None:
@@ -115,6 +128,14 @@ class Engine:
         self._next += 1
         self.queue.append(Request(rid, prompt, int(max_new), traj, None if stop is None else int(stop)))
         return rid
+
+    def _pages(self, prompt_len: int, max_new: int) -> int:
+        """Pages of a request at its longest: the last round writes a whole block behind its tokens."""
+        return -(-(prompt_len + max_new + self.B) // PAGE)
+
+    def _reserve(self, n: int):
+        """Pages for the block that the next call writes behind the first n slots' tokens."""
+        self.pool.resize(self.seq_len[:n], self.block_len[:n])
 
     def run(self) -> Dict[int, List[int]]:
         """Serves until every submitted request is finished; returns the
@@ -133,8 +154,16 @@ class Engine:
         torch, rt = self.rt.torch, self.rt
         new = []
         while self.queue and len(self.slots) < self.max_active:
+            if self.pool is not None:
+                need = self._pages(self.queue[0].prompt.size, self.queue[0].max_new)
+                if need > self.free_pages:
+                    break                             # until a request finishes
+                self.free_pages -= need
             req = self.queue.popleft()
             s = len(self.slots)
+            self.seq_len[s:s + 1].fill_(int(req.prompt.size))
+            if self.pool is not None:
+                self._reserve(s + 1)
             tok = torch.from_numpy(req.prompt).to(rt.device)
             if self.temperature is None:
                 rt.prefill(s, tok, self.anchor[s:s + 1])
@@ -142,7 +171,6 @@ class Engine:
                 self.streams[s:s + 1].fill_(req.rid)
                 one = rt.sampler(self.temperature, self.sampler.seed, self.streams[s:s + 1])
                 rt.prefill_sampled(s, tok, one, self.anchor[s:s + 1])
-            self.seq_len[s:s + 1].fill_(int(req.prompt.size))
             if req.traj is not None:
                 self._traj_row(s, req.traj)
             self.slots.append(req)
@@ -183,6 +211,8 @@ class Engine:
 
     def _round(self):
         rt, torch, n = self.rt, self.rt.torch, len(self.slots)
+        if self.pool is not None:
+            self._reserve(n)
         if self.temperature is not None:
             rt.draft_block(n, self.anchor, self.seq_len, self.carry_on, None, None, self.dl)
             rt.sample_draft(n, self.dl, self.anchor, self.seq_len, self.sampler, self.draft_tok, self.block)
@@ -240,6 +270,8 @@ class Engine:
             pt = rt.page_table
             idx = [s, last]
             pt[idx] = pt[[last, s]]
+            if self.pool is not None:
+                self.pool.n_held[idx] = self.pool.n_held[[last, s]]
             self.seq_len[s:s + 1].copy_(self.seq_len[last:last + 1])
             self.anchor[s:s + 1].copy_(self.anchor[last:last + 1])
             if self.traj is not None:
@@ -249,3 +281,7 @@ class Engine:
             rt.move_slot(last, s)
             self.slots[s] = self.slots[last]
         self.slots.pop()
+        if self.pool is not None:                     # the finished request's row is the last one now
+            self.free_pages += self._pages(req.prompt.size, req.max_new)
+            self.seq_len[last:last + 1].zero_()
+            self.pool.resize(self.seq_len[:last + 1])

@@ -123,6 +123,10 @@ EXPORTS = {
     "dflow_bench_force_drafts": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
                                                 ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "dflow_workspace_bytes_kv8": (ctypes.c_size_t, [ctypes.POINTER(Dims)]),
+    "dflow_create_kv8": (ctypes.c_int, [ctypes.POINTER(Dims), ctypes.POINTER(Weights), ctypes.POINTER(Cache),
+                                        ctypes.POINTER(KV8), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
+                                        ctypes.c_void_p, ctypes.POINTER(ctypes.c_void_p)]),
     "dflow_page_resize": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(Pool), ctypes.c_int, ctypes.c_void_p,
                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
                                          ctypes.c_void_p]),
@@ -180,11 +184,22 @@ def _stream():
 
 
 class Runtime:
-    """One DFlow context: uploaded/packed weights, paged KV pools, page table."""
+    """One DFlow context: uploaded/packed weights, paged KV pools, page table.
+
+    kv_cache "fp8" holds the target's cache in 8 bits (dflow_create_kv8;
+    kv8_layer(l) is layer l's KV8Cache).  num_pages sizes the pools; without
+    it every slot owns max_pages pages from the start.  With it the rows of the page
+    table start empty, and page_pool (a PagePool) gives them pages: the
+    caller (the Engine, for one) resizes them before prefill and draft_block."""
 
     def __init__(self, dims, block: int, max_batch: int, max_ctx: int, weights: Dict[str, np.ndarray],
-                 carry_window: str = "suffix", max_rows: int = 128, device: str = "cuda:0"):
+                 carry_window: str = "suffix", max_rows: int = 128, device: str = "cuda:0", kv_cache: str = "model",
+                 num_pages: Optional[int] = None):
         import torch
+        if kv_cache not in ("model", "fp8"):
+            raise DFlowError(f"kv_cache {kv_cache!r} (model: the model's storage type, or fp8)")
+        if num_pages is not None and num_pages < 1:
+            raise DFlowError(f"num_pages {num_pages} must be at least 1")
         if not torch.cuda.is_available():
             raise DFlowError("no HIP device available; the DFlow runtime has no CPU path")
         self.lib = load_library()
@@ -196,7 +211,7 @@ class Runtime:
         self.dtype_code = DFLOW_BF16 if dims.dtype == "bf16" else DFLOW_F32
         self.elt_torch = torch.int16 if dims.dtype == "bf16" else torch.float32
         self.max_pages = (max_ctx + 2 * block + PAGE - 1) // PAGE
-        self.num_pages = self.max_pages * max_batch
+        self.num_pages = self.max_pages * max_batch if num_pages is None else int(num_pages)
         self._keep: List = []
 
         d = Dims()
@@ -241,17 +256,32 @@ class Runtime:
 
         pool = self.num_pages * dims.n_kv_heads * PAGE * dims.head_dim
         z = lambda n: torch.zeros(n, dtype=self.elt_torch, device=self.device)
-        self.k_pool, self.v_pool = z(dims.n_layers * pool), z(dims.n_layers * pool)
         self.ck_pool, self.cv_pool = z(dims.n_draft_layers * pool), z(dims.n_draft_layers * pool)
-        pt = np.arange(self.num_pages, dtype=np.int32).reshape(max_batch, self.max_pages)
-        self.page_table = torch.from_numpy(pt).to(self.device)
         C = Cache()
-        C.k_pool, C.v_pool = self.k_pool.data_ptr(), self.v_pool.data_ptr()
+        self.kv8 = None
+        if kv_cache == "fp8":
+            shape = (dims.n_layers, self.num_pages, dims.n_kv_heads)
+            u8 = lambda *s: torch.zeros(*shape, *s, dtype=torch.uint8, device=self.device)
+            one = lambda: torch.ones(*shape, PAGE // 16, dtype=torch.float32, device=self.device)
+            self.kv8 = (u8(PAGE, dims.head_dim), u8(dims.head_dim, PAGE), one(), one())
+            self.ckv8 = KV8(*[t.data_ptr() for t in self.kv8], self.num_pages, dims.n_kv_heads, dims.head_dim)
+        else:
+            self.k_pool, self.v_pool = z(dims.n_layers * pool), z(dims.n_layers * pool)
+            C.k_pool, C.v_pool = self.k_pool.data_ptr(), self.v_pool.data_ptr()
+        self.page_pool = None
+        if num_pages is None:
+            pt = np.arange(self.num_pages, dtype=np.int32).reshape(max_batch, self.max_pages)
+            self.page_table = torch.from_numpy(pt).to(self.device)
+        else:
+            from .kv8 import PagePool
+            self.page_pool = PagePool.alloc(max_batch, self.max_pages, self.num_pages, self.device)
+            self.page_table = self.page_pool.page_table
         C.ck_pool, C.cv_pool = self.ck_pool.data_ptr(), self.cv_pool.data_ptr()
         C.page_table = self.page_table.data_ptr()
         self.ccache = C
         # workspace and status word: device memory owned here (torch), registered with the context
-        ws_bytes = int(self.lib.dflow_workspace_bytes(ctypes.byref(d)))
+        sizer = self.lib.dflow_workspace_bytes if self.kv8 is None else self.lib.dflow_workspace_bytes_kv8
+        ws_bytes = int(sizer(ctypes.byref(d)))
         if ws_bytes == 0:
             self._check(-2, "dflow_workspace_bytes")
         self.workspace = torch.empty(ws_bytes + 256, dtype=torch.uint8, device=self.device)
@@ -259,9 +289,20 @@ class Runtime:
         ws_ptr = (self.workspace.data_ptr() + 255) // 256 * 256
         torch.cuda.synchronize(self.device)
         ctx = ctypes.c_void_p()
-        self._check(self.lib.dflow_create(ctypes.byref(d), ctypes.byref(W), ctypes.byref(C), ws_ptr, ws_bytes,
-                                          self.status_word.data_ptr(), _stream(), ctypes.byref(ctx)), "dflow_create")
+        rest = (ws_ptr, ws_bytes, self.status_word.data_ptr(), _stream(), ctypes.byref(ctx))
+        if self.kv8 is None:
+            self._check(self.lib.dflow_create(ctypes.byref(d), ctypes.byref(W), ctypes.byref(C), *rest), "dflow_create")
+        else:
+            self._check(self.lib.dflow_create_kv8(ctypes.byref(d), ctypes.byref(W), ctypes.byref(C),
+                                                  ctypes.byref(self.ckv8), *rest), "dflow_create_kv8")
         self.ctx = ctx
+
+    def kv8_layer(self, l: int):
+        """The 8-bit cache of target layer l (kv_cache "fp8")."""
+        if self.kv8 is None:
+            raise DFlowError("the target cache is not held in 8 bits")
+        from .kv8 import KV8Cache
+        return KV8Cache(*[t[l] for t in self.kv8])
 
     # ------------------------------------------------------------ weights
     def _upload(self, a: np.ndarray):
