@@ -18,6 +18,7 @@
 namespace dflow {
 
 constexpr int KV8_GROUP = 16;
+constexpr long long KV8_MAX_WGS = (1ll << 24) - 1;     // of 256 threads: a launch has less than 2^32
 constexpr int KV8_MIN_EXP = -100, KV8_MAX_EXP = 120;   // exponents of the append's scales
 
 struct Kv8Cache {

@@ -926,7 +926,7 @@ static hipError_t launch_kv8_kernel(const Kv8AttnParams& p, const Kv8Split& sp, 
       hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (attr != hipSuccess) return attr;
   const long long wgs = (long long)p.nseq * p.c.Hkv * sp.tiles * sp.nsplit;
-  if (wgs > 0x7FFFFFFFll) return hipErrorInvalidConfiguration;
+  if (wgs > KV8_MAX_WGS) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(KERNEL, dim3((unsigned)wgs), dim3(threads), lds, st, p, sp);
   return hipGetLastError();
 }

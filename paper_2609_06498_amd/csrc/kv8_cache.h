@@ -183,10 +183,12 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
   static_assert(RC + 17 <= 64, "a lane per row of the window");
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool is_v = blockIdx.x & 1;            // units fastest: the heads of a row are read together
-  const int h = blockIdx.x >> 1;
-  const int r0 = (blockIdx.y * 4 + w) * RC;
-  if (r0 >= p.rows) return;                    // uniform per wave
+  const unsigned unit = blockIdx.x % (2u * p.c.Hkv);   // fastest: the heads of a row are read together
+  const bool is_v = unit & 1;
+  const int h = unit >> 1;
+  const unsigned first = (blockIdx.x / (2u * p.c.Hkv) * 4 + w) * RC;
+  if (first >= (unsigned)p.rows) return;       // uniform per wave
+  const int r0 = first;
   // slots of rows r0 - 1 (lane 0) .. r0 + RC + 15
   const int row = r0 - 1 + lane;
   const int cap = p.c.num_pages * PAGE;
@@ -198,7 +200,7 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
   const bool mine = lane >= 1 && lane <= RC;
   const bool follows = lane >= 1 && slot >= 0 && group == before;
   fault |= follows && slot <= sbefore;
-  if (blockIdx.x == 0 && __builtin_amdgcn_ballot_w64(mine && fault) != 0 && lane == 0) set_status(p.status, ST_BAD_SLOT);
+  if (unit == 0 && __builtin_amdgcn_ballot_w64(mine && fault) != 0 && lane == 0) set_status(p.status, ST_BAD_SLOT);
   uint64_t leads = __builtin_amdgcn_ballot_w64(mine && slot >= 0 && !follows);
   while (leads) {                              // uniform
     const int ld = __builtin_ctzll(leads);
@@ -240,15 +242,18 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
 // 16 rows; 15253 rows 36 us with 32, 29 with 16, 32 with 8), else one.
 constexpr int APPEND_RC = 16;
 
+template <typename T, int DH, int RC>
+static hipError_t launch_append_rc(const Kv8AppendParams& p, hipStream_t st) {
+  const long long wgs = 2ll * p.c.Hkv * (((long long)p.rows + 4 * RC - 1) / (4 * RC));
+  if (wgs > KV8_MAX_WGS) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((kv8_append_kernel<T, DH, RC>), dim3((unsigned)wgs), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
 template <typename T, int DH>
 static hipError_t launch_append_dh(const Kv8AppendParams& p, hipStream_t st) {
   // A round's rows spread over as many waves as there are rows; from a few
   // thousand rows on they are prompts, whose runs are 16 rows.
-  if (p.rows <= 2048)
-    hipLaunchKernelGGL((kv8_append_kernel<T, DH, 1>), dim3(2 * p.c.Hkv, (p.rows + 3) / 4), dim3(256), 0, st, p);
-  else
-    hipLaunchKernelGGL((kv8_append_kernel<T, DH, APPEND_RC>), dim3(2 * p.c.Hkv, (p.rows + 4 * APPEND_RC - 1) / (4 * APPEND_RC)), dim3(256), 0, st, p);
-  return hipGetLastError();
+  return p.rows <= 2048 ? launch_append_rc<T, DH, 1>(p, st) : launch_append_rc<T, DH, APPEND_RC>(p, st);
 }
 
 hipError_t launch_kv8_append(bool isbf, const Kv8AppendParams& p, hipStream_t st) {
@@ -418,8 +423,9 @@ __global__ void __launch_bounds__(256) slot_map_kernel(PageResizeParams p) {
   __shared__ int starts[PAGES_MAX_SEQ + 1];
   for (int i = threadIdx.x; i <= p.nseq; i += 256) starts[i] = p.row_start[i];
   __syncthreads();
-  const int r = blockIdx.x * 256 + threadIdx.x;
-  if (r >= starts[p.nseq]) return;
+  const unsigned at = blockIdx.x * 256 + threadIdx.x;
+  if (at >= (unsigned)starts[p.nseq]) return;
+  const int r = at;
   p.slot[r] = map_slot(p, starts, [&](int q) {
     const long long len = p.seq_len[q], more = p.new_len[q];
     return len < 0 || (len + more + PAGE - 1) / PAGE > p.n_held[q] ? -1 : (int)len;
@@ -434,7 +440,7 @@ hipError_t launch_page_resize(const PageResizeParams& p, hipStream_t st) {
   hipLaunchKernelGGL(page_resize_kernel, dim3(1), dim3(threads), 0, st, p, inl);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.slot || inl) return e;
-  hipLaunchKernelGGL(slot_map_kernel, dim3((p.slot_cap + 255) / 256), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(slot_map_kernel, dim3(((unsigned)p.slot_cap + 255u) / 256u), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 

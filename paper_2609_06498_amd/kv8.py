@@ -6,7 +6,7 @@ dflow_kv8_attention; the layouts are theirs (include/dflow.h).  The tensors
 belong to the caller and every call is asynchronous on torch's current stream
 of their device.  Calls through one KV8Cache share its workspace, so they must
 execute in order: one stream, or streams ordered by events; graphs captured
-through one cache are replayed one at a time.  What only the device can see
+through one cache are replayed one at a time, and the cache outlives them.  What only the device can see
 (a page id outside the pool, a sequence that does not fit) sets bits of the
 object's status word, which status() reads.
 """
@@ -101,6 +101,8 @@ class PagePool(_DeviceCalls):
         given = seq_len if new_len is None else (seq_len, new_len) if slot is None else (seq_len, new_len, slot, row_start)
         if slot is not None and (new_len is None or row_start is None):
             raise DFlowError("a slot map needs new_len and row_start")
+        if slot is None and row_start is not None:
+            raise DFlowError("row_start comes with a slot map")
         cap = 0 if slot is None else slot.numel()
         for t in (given if type(given) is tuple else (given,)):
             if t.dtype is not i32 or t.get_device() != i or t.dim() != 1 or not t.is_contiguous():
@@ -180,16 +182,19 @@ class KV8Cache(_DeviceCalls):
         need = self.lib.dflow_kv8_attention_workspace(*key, self.n_kv_heads, self.head_dim)
         if need == ctypes.c_size_t(-1).value:
             raise DFlowError(f"dflow_kv8_attention_workspace: {self.lib.dflow_last_error().decode()}")
-        if len(self._need) >= 4096:
-            self._need.clear()
-        self._need[key] = need
         if need > self._ws_bytes:
+            if self.torch.cuda.is_current_stream_capturing():
+                # (its first bytes would be zeroed by the graph's replays only)
+                raise DFlowError("this call's workspace must exist before it is captured: run it once first")
             if self._ws is not None:
                 self._kept.append(self._ws)
             self._ws_bytes = max(need, 2 * self._ws_bytes)
             self._ws = self.torch.empty(self._ws_bytes, dtype=self.torch.uint8, device=self.device)
             self._ws[:WORKSPACE_ZEROED].zero_()
             self._ws_ptr = self._ws.data_ptr()
+        if len(self._need) >= 4096:
+            self._need.clear()
+        self._need[key] = need
 
     def attention(self, q, page_table, kv_len, row_start, max_rows: int, max_len: int, causal: bool = True,
                   scale: Optional[float] = None, out=None):
