@@ -84,6 +84,7 @@ class Engine:
         if self.pool is not None:
             self.block_len = torch.full((n,), B, dtype=torch.int32, device=dev)
             self.free_pages = rt.num_pages            # beyond what active requests may come to need
+            self.pool.resize(self.seq_len)            # empty rows, whatever an earlier engine left in them
         self.force_mean = force_mean
         self.seed = seed
         self.temperature = temperature

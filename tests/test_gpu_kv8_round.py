@@ -225,3 +225,31 @@ def test_round_over_the_8_bit_cache_captured():
     for a, b in zip(*runs):
         np.testing.assert_array_equal(a[0], b[0])
         np.testing.assert_array_equal(a[1], b[1])
+
+
+def test_an_engine_after_one_that_was_given_up():
+    """A pool's pages belong to the engine that was built last."""
+    from paper_2609_06498_amd import Runtime
+    from paper_2609_06498_amd.engine import Engine
+    wl = get_config("tiny-f32")
+    w = make_weights(wl.dims, wl.seed_w)
+    rng = np.random.default_rng(4)
+    prompts = [rng.integers(0, wl.dims.vocab, n).astype(np.int32) for n in (150, 90, 120)]
+    outs = []
+    for given_up in (False, True):
+        rt = Runtime(wl.dims, wl.block, 3, 400, w, kv_cache="fp8", num_pages=9)
+        if given_up:
+            eng = Engine(rt)
+            for p in prompts[1:]:
+                eng.submit(p, 30)
+            eng._admit()
+            torch.cuda.synchronize()
+            assert int(rt.page_pool.n_free) < 9
+        eng = Engine(rt)
+        rids = [eng.submit(p, 12) for p in prompts]
+        got = eng.run()
+        torch.cuda.synchronize()
+        assert rt.status() == 0 and eng.pool.status() == 0 and int(eng.pool.n_free) == 9
+        outs.append([got[r] for r in rids])
+        rt.close()
+    assert outs[0] == outs[1]
