@@ -165,8 +165,8 @@ struct Kv8Query {
 // to 224..448.  Eight significant bits are four and, signed, four more: exact for
 // elements down to 2^-10 of the row's largest, smaller ones are off by at most
 // 2^-18 of it (the subnormal step).  The key codes then go to the 128-deep e4m3
-// product as they were stored: no conversions, whose vector operations bound the
-// loop with bf16 operands (64 of 354 a page and wave), at the same matrix time.
+// product as they were stored: no conversions (64 of 354 vector operations a page and
+// wave with bf16 operands), at the same matrix time.
 template <int DH>
 struct Kv8Query<bf16, DH> {
   static constexpr int KI = DH / 64;
@@ -363,7 +363,7 @@ __device__ __forceinline__ float2 kv8_get2(const float* p) {
 // workgroups to arrive (a counter each, zero between launches) merges all of them
 // in split order; partials then are written and read at device scope, since these
 // workgroups may run on different XCDs, whose caches are not coherent.  (4096 keys, one
-// row: 14.3 -> 11.6 us against a launch for it.)  More rows: the combine kernel,
+// row: 14.3 -> 11.6 us against a launch for it when added.)  More rows: the combine kernel,
 // since one workgroup would read all of a tile's partials (64 rows of 32 splits: 17.4
 // against 40 us).
 template <typename T, int DH, int RG, int TW, int PW>
@@ -835,13 +835,30 @@ __global__ void __launch_bounds__(KV8_SHARED_WAVES * 64, 2) kv8_shared_kernel(Kv
   kv8_finish<T, DH, RG, TW, PW>(p, sp, it, r0, tw, pw, kv8_smem, w.M, w.l, w.o);
 }
 
-// Merges the splits of one 16-row group in split order: wave d the 16 channels
-// of output tile d, in the accumulator order the partials were left in.
-template <typename T, int DH>
+// Merges the splits of one 16-row group in split order, U splits' loads in flight
+// together: wave d the 16 channels of output tile d, in the accumulator order the
+// partials were left in.  Two splits, as a prompt chunk may have, load no more than
+// two (1024-row chunk: 15.6 us with eight loads, six of them the second split again,
+// 10.6 with two; the whole call 116.5 -> 110).
+template <typename T, int DH, int U>
 __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams p, Kv8Split sp) {
+  constexpr int REC = 16 * DH + 32;
   const int lane = threadIdx.x & 63, d = threadIdx.x >> 6;
   const int Hkv = p.c.Hkv, G = p.Hq / Hkv, tile_rg = sp.tw * sp.rg, rgs = sp.tiles * tile_rg;
   const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, rg = rest % rgs, s = rest / rgs;
+  const float* rec = p.part + KV8_COUNTERS + (((size_t)s * Hkv + kvh) * rgs + rg) * sp.nsplit * REC;
+  const float* pv = rec + (d * 64 + lane) * 4;
+  const float* pm = rec + 16 * DH + 2 * (lane & 15);
+  float2 ml[U];
+  float4 v[U];
+  auto load = [&](int i, int last) {           // (past the last split: it again, unused)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (size_t)min(i + u, last) * REC;
+      ml[u] = *reinterpret_cast<const float2*>(pm + at);
+      v[u] = *reinterpret_cast<const float4*>(pv + at);
+    }
+  };
   Kv8Rows rows;
   int bits;
   if (!kv8_rows(p, s, rows, bits)) return;
@@ -850,28 +867,17 @@ __global__ void __launch_bounds__(DH / 16 * 64) kv8_combine_kernel(Kv8AttnParams
   const int tile_end = min((rg / tile_rg + 1) * tile_rg * 16, R);
   const int nact = kv8_active(rows.limit((tile_end - 1) / G, p.causal), sp.split_pages);
   if (nact == 1) return;
-  const float* rec = p.part + KV8_COUNTERS + (((size_t)s * Hkv + kvh) * rgs + rg) * sp.nsplit * (16 * DH + 32);
   const int r = rg * 16 + (lane & 15);
-  constexpr int REC = 16 * DH + 32, U = 8;
-  const float* pv = rec + (d * 64 + lane) * 4;
-  const float* pm = rec + 16 * DH + 2 * (lane & 15);
   float M = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < nact; i += U) {          // U splits' loads in flight together (past the last: it again, unused)
-    float2 ml[U];
-    float4 v[U];
+  for (int i = 0; i < nact; i += U) {
+    load(i, nact - 1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const size_t at = (size_t)min(i + u, nact - 1) * REC;
-      ml[u] = *reinterpret_cast<const float2*>(pm + at);
-      v[u] = *reinterpret_cast<const float4*>(pv + at);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float mi = i + u < nact ? ml[u].x : -INFINITY;
+      const bool on = i + u < nact;            // (NaN of a partial stays NaN, an unused one adds nothing)
+      const float mi = on ? ml[u].x : -INFINITY;
       const float mn = fmaxf(M, mi);
       const float f1 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
       const float f2 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mn);
-      const bool on = i + u < nact;            // (NaN of a partial stays NaN, an unused one adds nothing)
       l = l * f1 + (on ? ml[u].y * f2 : 0.f);
       y[0] = y[0] * f1 + (on ? v[u].x * f2 : 0.f);
       y[1] = y[1] * f1 + (on ? v[u].y * f2 : 0.f);
@@ -930,9 +936,9 @@ static hipError_t launch_kv8_kernel(const Kv8AttnParams& p, const Kv8Split& sp, 
   hipLaunchKernelGGL(KERNEL, dim3((unsigned)wgs), dim3(threads), lds, st, p, sp);
   return hipGetLastError();
 }
-template <typename T, int DH>
+template <typename T, int DH, int U>
 static hipError_t launch_kv8_combine(const Kv8AttnParams& p, const Kv8Split& sp, hipStream_t st) {
-  hipLaunchKernelGGL((kv8_combine_kernel<T, DH>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.tw * sp.rg), dim3(DH * 4), 0, st,
+  hipLaunchKernelGGL((kv8_combine_kernel<T, DH, U>), dim3(p.nseq * p.c.Hkv * sp.tiles * sp.tw * sp.rg), dim3(DH * 4), 0, st,
                      p, sp);
   return hipGetLastError();
 }
@@ -952,7 +958,8 @@ static hipError_t launch_kv8_shared(const Kv8AttnParams& p, const Kv8Split& sp, 
   constexpr size_t merge = kv8_merge_bytes(DH, RG, TW, PW);
   const hipError_t e =
       launch_kv8_kernel<&kv8_shared_kernel<T, DH, RG, TW>>(p, sp, KV8_SHARED_WAVES * 64, ring > merge ? ring : merge, st);
-  return e != hipSuccess || sp.nsplit == 1 ? e : launch_kv8_combine<T, DH>(p, sp, st);
+  if (e != hipSuccess || sp.nsplit == 1) return e;
+  return sp.nsplit == 2 ? launch_kv8_combine<T, DH, 2>(p, sp, st) : launch_kv8_combine<T, DH, 8>(p, sp, st);
 }
 
 template <typename T, int DH>

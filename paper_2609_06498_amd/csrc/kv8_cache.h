@@ -239,7 +239,8 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(Kv8AppendParams p) {
 }
 
 // Lanes find their rows' runs 16 to a wave where there are many (prompts: a run is
-// 16 rows; 15253 rows 36 us with 32, 29 with 16, 32 with 8), else one.
+// 16 rows; 15253 rows 36 us with 32, 29 with 16, 32 with 8, before whole groups had a path of
+// their own: now 24), else one.
 constexpr int APPEND_RC = 16;
 
 template <typename T, int DH, int RC>
