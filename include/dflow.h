@@ -493,7 +493,8 @@ size_t dflow_kv8_attention_workspace(int dtype, int nseq, int max_rows, int max_
  * DFLOW_STATUS_CAPACITY.  Keys of a page whose id is outside the pool are not
  * seen (DFLOW_STATUS_BAD_PAGE).  Bytes behind a sequence's end may be anything.
  * Scores, sums and outputs are held in fp32; bf16 rows round probabilities to 11
- * bits, fp32 rows to 22.  workspace: device, 16-byte aligned, its first
+ * bits and query elements below 2^-10 of the row's largest in magnitude to 2^-18 of it,
+ * fp32 rows probabilities to 22 bits.  workspace: device, 16-byte aligned, its first
  * DFLOW_KV8_WORKSPACE_ZEROED bytes zero before its first call (every call leaves
  * them zero), used by one call at a time (calls and graphs that share it must
  * not overlap). */
